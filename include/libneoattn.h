@@ -462,6 +462,173 @@ neo_status neo_sched_step(neo_sched* s, neo_sched_iter* info, int64_t* ids, int6
 neo_status neo_sched_get_stats(const neo_sched* s, neo_sched_stats* out);
 void neo_sched_destroy(neo_sched* s);
 
+/* ------------------------------------------------------------------------
+ * Decode attention with shaped scores, and what keeps the cache small: a cache
+ * held in 4 bits, and eviction by accumulated attention weight.
+ *
+ * A request b of L cached tokens sees the tokens t < L with t < prefix_lens[b]
+ * or t >= starts[b]. For query head h of kv head g, a token's score is
+ *
+ *   x_t = scale * q[b][h] . K[b][g][t]
+ *   x_t = softcap * tanh(x_t / softcap)          (softcap > 0)
+ *   x_t = x_t + slopes[h] * (t - (L - 1))        (slopes given)
+ *
+ * so a positive slope makes distant tokens count less. starts is the first
+ * token of a window or of the request's own document, prefix_lens the length
+ * of a prefix (or of the first tokens) that is seen besides; both are clamped
+ * to [0, L]. A request that sees nothing gets zero rows and a log-sum-exp of
+ * minus infinity. Blocks without a token that is seen are not read.
+ * Distances count cache slots: after an eviction, the tokens that are left.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+  float softcap;              /* 0: none */
+  const float* slopes;        /* device [num_q_heads], or NULL: no bias; finite */
+  const int32_t* starts;      /* device [batch], or NULL: 0 */
+  const int32_t* prefix_lens; /* device [batch], or NULL: 0 */
+} neo_score_shape;
+
+/*
+ * neo_decode_attention_ex with shaped scores (shape may be NULL: plain ones).
+ * lse: device fp32 [batch][num_q_heads], the natural logarithm of each row's
+ * sum of exponentials, or NULL. q, out, the caches, kv_block_stride, the
+ * limits, the clamping rules and the workspace (size, zero fill, one per call
+ * that may overlap) are those of neo_decode_attention_ex; a workspace may serve
+ * both calls in turn. NEO_ERR_INVALID_ARG for a softcap that is negative or not
+ * finite, or when scale / softcap is not finite.
+ */
+neo_status neo_shaped_decode_attention(const void* q, const void* k_cache, const void* v_cache,
+                                       const int32_t* block_table, const int32_t* seq_lens,
+                                       int32_t num_q_heads, int32_t num_kv_heads,
+                                       int32_t head_dim, int32_t block_size, float scale,
+                                       const neo_score_shape* shape, float* out, float* lse,
+                                       int32_t batch, int32_t max_blocks_per_seq,
+                                       int32_t num_blocks, int64_t kv_block_stride,
+                                       void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The packed cache: K and V of a block and kv head are one record of
+ * NEO_PACKED_RECORD_BYTES bytes, [num_blocks][num_kv_heads][record], 0.27 of
+ * the two bf16 tiles. Values are 4-bit numbers (a sign and 0, 0.5, 1, 1.5, 2,
+ * 3, 4 or 6; codes 0-7, plus 8 if negative) times a power of two that 32
+ * consecutive dims of a token share. Its exponent e is the smallest in
+ * [-125, 125] for which the largest magnitude is below 7 * 2^e, stored as the
+ * byte e + 127; 0 if all 32 values are zero, 255 if one is infinite or NaN (all
+ * of them then read as NaN). Values are rounded to the nearest number, ties to
+ * the even code. In the record:
+ *   K, byte 0:          [4 dim groups][16 tokens][16 bytes], byte j of a run the
+ *                       dims 2j (low half) and 2j + 1 of the group
+ *   V, byte 1024:       [4 token groups][16 dim octets][4 tokens][4 bytes]
+ *   K exponents, 2048:  [4 dim groups][16 tokens]
+ *   V exponents, 2112:  [4 token groups][4 dim groups][4 tokens]
+ * Block tables are those of the bf16 caches. block_stride: bytes from one block
+ * to the next, 0 for dense (num_kv_heads * record), else a multiple of 16 of at
+ * least that and at most 2^40, the cache spanning less than 2^61 bytes
+ * (NEO_ERR_INVALID_ARG). The cache must be 16-byte aligned.
+ */
+#define NEO_PACKED_RECORD_BYTES 2176
+
+/* neo_shaped_decode_attention over a packed cache: the attention of the values
+ * that the cache stands for, computed as for a bf16 cache. */
+neo_status neo_packed_decode_attention(const void* q, const void* cache,
+                                       const int32_t* block_table, const int32_t* seq_lens,
+                                       int32_t num_q_heads, int32_t num_kv_heads,
+                                       int32_t head_dim, int32_t block_size, float scale,
+                                       const neo_score_shape* shape, float* out, float* lse,
+                                       int32_t batch, int32_t max_blocks_per_seq,
+                                       int32_t num_blocks, int64_t block_stride, void* workspace,
+                                       size_t workspace_bytes, void* stream);
+
+/*
+ * Append `rows` new tokens to a packed cache. Request b's are rows
+ * row_starts[b] .. row_starts[b + 1] - 1 of k_new and v_new (device int32
+ * [batch + 1], ascending; NULL: one row per request, rows = batch), and they
+ * become its last tokens: the last of them token seq_lens[b] - 1 (seq_lens
+ * counts them). k_new, v_new: device bf16, row r and kv head g at
+ * r * row_stride + g * head_stride, 128 values in a run; strides in elements,
+ * multiples of 8 from 0 to 2^30, pointers 16-byte aligned. Rows past
+ * row_starts[batch] and rows before token 0 are skipped, lengths past the table
+ * are clamped to it, and a block id outside [0, num_blocks) skips its rows.
+ * rows * num_kv_heads must stay below 2^31.
+ */
+neo_status neo_packed_append(void* cache, const void* k_new, const void* v_new,
+                             const int32_t* row_starts, int32_t rows, int64_t k_row_stride,
+                             int64_t k_head_stride, int64_t v_row_stride, int64_t v_head_stride,
+                             const int32_t* block_table, const int32_t* seq_lens, int32_t batch,
+                             int32_t max_blocks_per_seq, int32_t num_kv_heads, int32_t head_dim,
+                             int32_t block_size, int32_t num_blocks, int64_t block_stride,
+                             void* stream);
+
+/*
+ * Read tokens of a packed cache back as bf16, exactly: the rows that
+ * neo_packed_append with the same row_starts and lengths would write, to k_out
+ * and v_out (device bf16 [rows][num_kv_heads][128]). With row_starts the prefix
+ * sums of seq_lens, the whole cache. Rows that have no token keep what they
+ * held; block ids are clamped as for neo_decode_attention.
+ */
+neo_status neo_packed_gather(const void* cache, const int32_t* row_starts, int32_t rows,
+                             const int32_t* block_table, const int32_t* seq_lens, int32_t batch,
+                             int32_t max_blocks_per_seq, int32_t num_kv_heads, int32_t head_dim,
+                             int32_t block_size, int32_t num_blocks, int64_t block_stride,
+                             void* k_out, void* v_out, void* stream);
+
+/*
+ * Add one step's attention weights to running sums, the measure by which
+ * neo_kv_evict keeps tokens: for every token t that request b sees,
+ *   sums_out[b][g][t] = sums[b][g][t] + sum over h of kv head g of exp(x_t - lse[b][h])
+ * with the scores above and the log-sum-exps that neo_shaped_decode_attention
+ * wrote for the same arguments. sums, sums_out: device fp32
+ * [batch][num_kv_heads][sums_stride], the same buffer or two that do not
+ * overlap; other elements of sums_out are left as they are. sums_stride: at
+ * least max_blocks_per_seq * block_size. Reads K alone; no workspace.
+ */
+neo_status neo_add_attention_weights(const float* sums, float* sums_out, int64_t sums_stride,
+                                     const float* lse, const void* q, const void* k_cache,
+                                     const int32_t* block_table, const int32_t* seq_lens,
+                                     int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                                     int32_t block_size, float scale,
+                                     const neo_score_shape* shape, int32_t batch,
+                                     int32_t max_blocks_per_seq, int32_t num_blocks,
+                                     int64_t kv_block_stride, void* stream);
+neo_status neo_packed_add_attention_weights(const float* sums, float* sums_out,
+                                            int64_t sums_stride, const float* lse, const void* q,
+                                            const void* cache, const int32_t* block_table,
+                                            const int32_t* seq_lens, int32_t num_q_heads,
+                                            int32_t num_kv_heads, int32_t head_dim,
+                                            int32_t block_size, float scale,
+                                            const neo_score_shape* shape, int32_t batch,
+                                            int32_t max_blocks_per_seq, int32_t num_blocks,
+                                            int64_t block_stride, void* stream);
+
+/*
+ * Evict tokens by accumulated attention weight. Of request b's L tokens,
+ * n = min(L, budgets[b], 16 * new_blocks_per_seq) stay (budgets: device int32
+ * [batch], negative: 0): the newest min(recent, n), and for each kv head of its
+ * own the tokens with the largest sums among the others (equal sums: the lower
+ * token; a NaN is the largest). They are copied in their order to the blocks
+ * new_table[b] (device int32 [batch][new_blocks_per_seq]) of the same caches;
+ * the slots after them in the last block become zero. Blocks that block_table
+ * names are only read, so requests may share them; the new blocks must be
+ * distinct and none of those. Ids outside [0, num_blocks) in new_table skip
+ * their block.
+ * Writes new_lens [batch] = n, and [batch][num_kv_heads][16 * new_blocks_per_seq]:
+ * kept, the tokens' former positions, then -1; new_sums, their sums, then 0.
+ * sums and sums_stride as for neo_add_attention_weights.
+ */
+neo_status neo_kv_evict(void* k_cache, void* v_cache, const int32_t* block_table,
+                        const int32_t* seq_lens, const float* sums, int64_t sums_stride,
+                        const int32_t* budgets, int32_t recent, const int32_t* new_table,
+                        int32_t new_blocks_per_seq, int32_t* new_lens, int32_t* kept,
+                        float* new_sums, int32_t batch, int32_t max_blocks_per_seq,
+                        int32_t num_kv_heads, int32_t head_dim, int32_t block_size,
+                        int32_t num_blocks, int64_t kv_block_stride, void* stream);
+neo_status neo_packed_evict(void* cache, const int32_t* block_table, const int32_t* seq_lens,
+                            const float* sums, int64_t sums_stride, const int32_t* budgets,
+                            int32_t recent, const int32_t* new_table, int32_t new_blocks_per_seq,
+                            int32_t* new_lens, int32_t* kept, float* new_sums, int32_t batch,
+                            int32_t max_blocks_per_seq, int32_t num_kv_heads, int32_t head_dim,
+                            int32_t block_size, int32_t num_blocks, int64_t block_stride,
+                            void* stream);
+
 /*
  * Opt-in check of the indexing inputs: counts seq_lens outside
  * [0, max_blocks_per_seq * block_size] and block-table entries in use

@@ -36,6 +36,9 @@ __all__ = [
     "cpu_best_isa", "cpu_default_threads", "cpu_read_probe", "cpu_kv_append",
     "read_probe", "read_probe_tiles", "READ_PROBE_SINK_WORDS", "new_kv_cache",
     "debug_division", "DIVISIONS",
+    "shaped_decode_attention", "packed_decode_attention", "new_packed_kv_cache",
+    "packed_append", "packed_gather", "add_attention_weights",
+    "packed_add_attention_weights", "kv_evict", "packed_evict", "PACKED_RECORD_BYTES",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -139,6 +142,7 @@ def load_library():
         lib.neo_last_error.restype = ctypes.c_char_p
         lib.neo_version.argtypes = []
         lib.neo_version.restype = ctypes.c_char_p
+        shaped.declare(lib)
         _lib = lib
     return _lib
 
@@ -625,3 +629,10 @@ def cpu_kv_append(k_cache, v_cache, k_new, v_new, block_table, seq_lens):
         raise ValueError("k_new and v_new must be [batch, num_kv_heads, head_dim]")
     _check(lib.neo_cpu_kv_append(kp, vp, knp, vnp, bp, lp, B, block_table.shape[1], Hkv,
                                  npieces * x, bs, NB))
+
+
+from . import shaped  # noqa: E402  (it uses the functions above)
+from .shaped import (  # noqa: E402
+    PACKED_RECORD_BYTES, add_attention_weights, kv_evict, new_packed_kv_cache,
+    packed_add_attention_weights, packed_append, packed_decode_attention, packed_evict,
+    packed_gather, shaped_decode_attention)

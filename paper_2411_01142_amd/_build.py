@@ -14,7 +14,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libneoattn.so")
 BUILD_DIR = os.path.join(PKG, "_build")
 
-SOURCES = ["api.hip", "plan_combine.hip", "decode_mfma.hip", "decode_valu.hip", "kv_ops.hip"]
+SOURCES = ["api.hip", "plan_combine.hip", "decode_mfma.hip", "decode_valu.hip", "kv_ops.hip",
+           "api_shaped.hip", "shaped_bf16.hip", "shaped_packed.hip", "packed_ops.hip", "evict.hip"]
 # Host-only C++ (the CPU attention, the scheduler, the error text), built with
 # the host compiler; the CPU attention's ISA-specific functions carry target
 # attributes and are picked at run time.

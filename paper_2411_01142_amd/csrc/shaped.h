@@ -1,0 +1,574 @@
+// Decode attention with shaped scores: what the kernels over bf16 and packed
+// caches share. For request b, L = lens[b], query head h and a token t that it
+// sees (t < prefix[b] or t >= starts[b], below L):
+//
+//   x_t = scale * q_h . k_t;   x_t = cap * tanh(x_t / cap);   x_t += slope_h * (t - (L - 1))
+//   out_h = sum_t exp(x_t - max x) v_t / sum_t exp(x_t - max x),   lse_h = log sum_t exp(x_t)
+//
+// Blocks without a token that is seen are neither read nor counted as work.
+#pragma once
+
+#include "decode_common.h"
+#include "packed.h"
+
+namespace neo {
+
+struct ShapedParams {
+  const uint16_t* q;        // [batch][hq][128] bf16
+  const uint8_t* k;         // K of the bf16 cache, or the packed cache
+  const uint8_t* v;         // V of the bf16 cache
+  int64_t blk_bytes;        // bytes from one block to the next
+  const int32_t* table;     // [batch][mbps]
+  const int32_t* lens;      // [batch]
+  const int32_t* starts;    // [batch] or null: 0
+  const int32_t* prefix;    // [batch] or null: 0
+  const float* slopes;      // [hq] or null: 0
+  float* out;               // [batch][hq][128]
+  float* lse;               // [batch][hq] or null
+  float* part_o;            // partial rows, a slot of [group][128] each
+  float* part_ml;           // their maxima and denominators, [group][2]
+  int32_t* counters;        // arrivals, zero between calls
+  const float* sums;        // weight sums [batch][hkv][sums_stride], read
+  float* sums_out;          // and written
+  const float* lse_in;      // [batch][hq]
+  int64_t sums_stride;
+  int32_t batch, hq, hkv, mbps, num_blocks;
+  int32_t parts;            // workgroups of a (request, kv head) pair, at most
+  float scale_log2;         // scale * log2(e)
+  float cap_in, cap_log2;   // scale / cap and cap * log2(e); cap_log2 0: no cap
+};
+
+// What a request sees: tokens [0, p) and [s, L), in n blocks: the first pb, and
+// those from block f on. Virtual block j is block_of(j) of the table row.
+struct Seen {
+  int32_t L, p, s, pb, f, n;
+  __device__ int32_t block_of(int32_t j) const { return j < pb ? j : j - pb + f; }
+  __device__ bool sees(int32_t t) const { return t < L && (t < p || t >= s); }
+  __device__ int32_t first() const { return p > 0 ? 0 : s; }
+  // Whether all tokens of the k virtual blocks from j on are seen.
+  __device__ bool sees_all(int32_t j, int32_t k) const {
+    return (j + k) * kBlock <= p ||
+           (j >= pb && (j - pb + f) * kBlock >= s && (j + k - pb + f) * kBlock <= L);
+  }
+};
+__device__ inline Seen make_seen(int32_t len, int32_t start, int32_t prefix, int32_t mbps) {
+  Seen v;
+  v.L = clamp_len(len, mbps);
+  v.p = min(max(prefix, 0), v.L);
+  v.s = min(max(start, v.p), v.L);
+  if (v.s == v.p) v.s = v.p = 0;  // one range
+  v.pb = (v.p + kBlock - 1) / kBlock;
+  const int32_t nb = (v.L + kBlock - 1) / kBlock;
+  v.f = v.s < v.L ? max(v.s / kBlock, v.pb) : nb;
+  v.n = v.pb + nb - v.f;
+  return v;
+}
+__device__ inline Seen load_seen(const ShapedParams& p, int32_t b) {
+  return make_seen(p.lens[b], p.starts ? p.starts[b] : 0, p.prefix ? p.prefix[b] : 0, p.mbps);
+}
+__device__ inline Seen make_uniform(Seen v) {
+  v.L = uniform(v.L);
+  v.p = uniform(v.p);
+  v.s = uniform(v.s);
+  v.pb = uniform(v.pb);
+  v.f = uniform(v.f);
+  v.n = uniform(v.n);
+  return v;
+}
+
+// Wave-uniform reads of the block table through the scalar cache: they neither
+// occupy vector registers nor stand in the queue of the tile loads, whose
+// in-order wait counts they would lengthen.
+typedef const __attribute__((address_space(4))) int32_t* ScalarInts;
+__device__ inline ScalarInts scalar_ints(const int32_t* p) { return (ScalarInts)(uintptr_t)p; }
+
+__device__ inline __amdgpu_buffer_rsrc_t bytes_rsrc(const uint8_t* base, int32_t bytes) {
+  const uint64_t a = reinterpret_cast<uint64_t>(base);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)a);
+  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32));
+  void* u = reinterpret_cast<void*>(((uint64_t)hi << 32) | lo);
+  return __builtin_amdgcn_make_buffer_rsrc(u, (short)0, uniform(bytes), kBufferWord3);
+}
+
+// Lane l's value from lane l ^ 8 (a rotation of each 16-lane row by eight).
+constexpr int kDppRowRor8 = 0x128;
+__device__ inline uint32_t from_xor8(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kDppRowRor8, 0xF, 0xF, true);
+}
+__device__ inline float from_xor8(float v) {
+  return __builtin_bit_cast(float, from_xor8(__builtin_bit_cast(uint32_t, v)));
+}
+
+// tanh to fp32 accuracy in the absolute sense that scores need: odd Taylor
+// polynomial below 0.3 (the first term left out is 1e-8 of the value there),
+// from the exponential above, where 1 - 2 / (e^2y + 1) cancels little.
+__device__ inline float tanh_score(float y) {
+  const float y2 = y * y;
+  float r = fmaf(y2, -1382.f / 155925.f, 62.f / 2835.f);
+  r = fmaf(y2, r, -17.f / 315.f);
+  r = fmaf(y2, r, 2.f / 15.f);
+  r = fmaf(y2, r, -1.f / 3.f);
+  const float small = fmaf(y * y2, r, y);
+  const float e = __builtin_amdgcn_exp2f(fabsf(y) * 2.8853900817779268f);  // e^(2|y|)
+  const float big = copysignf(1.f - 2.f * __builtin_amdgcn_rcpf(e + 1.f), y);
+  return fabsf(y) < 0.3f ? small : big;
+}
+
+// ------------------------------------------------------------------ caches
+
+// A cache type provides the matrix products over a step of kStep blocks. Each
+// lane holds kValues scores of one head; position() tells which tokens they are.
+//
+// bf16: one block a step, the layouts and products of the plain decode kernel.
+template <int G_>
+struct Bf16Cache {
+  static constexpr int G = G_;
+  static constexpr int kStep = 1;
+  static constexpr int kValues = 4;
+  static constexpr int kHeadBytes = kTileBytes;
+  struct Tile {
+    bf16x8_t k[4];
+    s16x4_t v[8];
+  };
+  struct Q {
+    bf16x8_t f[4];
+  };
+  __device__ static int head(int lane) { return lane & 15; }
+  __device__ static void load_q(Q& q, const uint16_t* __restrict__ rows, int lane) {
+    const int h = head(lane), rq = lane >> 4;
+    const uint16_t* row = rows + (h < G ? h : 0) * kHeadDim;
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb)
+      q.f[kb] = *reinterpret_cast<const bf16x8_t*>(row + kPiece * (4 * kb + rq));
+  }
+  template <bool kV>
+  __device__ static void load(Tile& x, int, const ShapedParams& p, size_t off, bool valid,
+                              int lane) {
+    const int col = lane & 15, rq = lane >> 4;
+    const __amdgpu_buffer_rsrc_t rk = bytes_rsrc(p.k + off, valid ? kTileBytes : 0);
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb)
+      x.k[kb] = __builtin_bit_cast(bf16x8_t, tile_load16(rk, 2 * kPiece * (kWave * kb + lane)));
+    if constexpr (kV) {
+      const __amdgpu_buffer_rsrc_t rv = bytes_rsrc(p.v + off, valid ? kTileBytes : 0);
+#pragma unroll
+      for (int mb = 0; mb < 8; ++mb)
+        x.v[mb] = tile_load8(rv, 2 * ((16 * mb + col) * kBlock + 4 * rq));
+    }
+  }
+  __device__ static void scores(const Tile& x, const Q& q, float (&s)[kValues], int) {
+    f32x4_t a = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb)
+      a = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.k[kb], q.f[kb], a, 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] = a[i];
+  }
+  // First token of the four in s[4v .. 4v + 3].
+  __device__ static int32_t position(int, const int32_t (&first)[kStep], int lane) {
+    return first[0] + 4 * (lane >> 4);
+  }
+  __device__ static void hide_value(Tile& x, int, int i) {
+#pragma unroll
+    for (int mb = 0; mb < 8; ++mb) x.v[mb][i] = 0;
+  }
+  __device__ static float head_max(float v) { return max_over_rows(v); }
+  __device__ static float head_sum(float v) { return sum_over_rows(v); }
+  // Weights enter the product as bf16 hi + lo halves, about 16 bits of each.
+  __device__ static void add_values(f32x4_t (&acc)[8], const Tile& x, const float (&w)[kValues],
+                                    int) {
+    s16x4_t hi, lo;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __bf16 h = (__bf16)w[i];
+      hi[i] = __builtin_bit_cast(short, h);
+      lo[i] = __builtin_bit_cast(short, (__bf16)(w[i] - (float)h));
+    }
+#pragma unroll
+    for (int mb = 0; mb < 8; ++mb) {
+      acc[mb] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(x.v[mb], hi, acc[mb], 0, 0, 0);
+      acc[mb] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(x.v[mb], lo, acc[mb], 0, 0, 0);
+    }
+  }
+  __device__ static void fold(f32x4_t (&)[8]) {}
+  // Word c (dims 4c .. 4c + 3) of this lane's head, for its eight words.
+  template <class Fn>
+  __device__ static void each_word(const f32x4_t (&acc)[8], int lane, Fn fn) {
+#pragma unroll
+    for (int mb = 0; mb < 8; ++mb) fn(4 * mb + (lane >> 4), acc[mb]);
+  }
+};
+
+// Packed: four blocks a step (64 tokens, 8.5 KiB, as much as a bf16 block), so
+// that the running maximum, the rescaling and the addresses are paid once for 64
+// tokens. Records become bf16 in registers, a pair of values an instruction.
+//
+// With up to eight heads a matrix product's 16 columns hold them twice. Of the
+// scores of two blocks, lanes of columns 0-7 keep the first block's and those of
+// columns 8-15 the second's, so that half as many are left to each lane; and in
+// the second product columns 0-7 carry the weights' bf16 hi halves and 8-15 the
+// lo halves, so that one product does the work of two. The lanes exchange the
+// halves that the other needs with a rotation by eight.
+template <int G_>
+struct PackedCache {
+  static constexpr int G = G_;
+  static constexpr int kStep = 4;
+  static constexpr bool kTwice = G <= 8;
+  static constexpr int kValues = kTwice ? 8 : 16;
+  static constexpr int kHeadBytes = kPackedRecord;
+  struct Tile {
+    u32x4_t k[kStep], v[kStep];
+    uint32_t ke[kStep], ve[kStep];  // exponent bytes: of the K run, of four V tokens
+  };
+  struct Q {
+    bf16x8_t f[4];
+  };
+  __device__ static int head(int lane) { return lane & (kTwice ? 7 : 15); }
+  __device__ static void load_q(Q& q, const uint16_t* __restrict__ rows, int lane) {
+    const int h = head(lane), rq = lane >> 4;
+    const uint16_t* row = rows + (h < G ? h : 0) * kHeadDim;
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb)
+      q.f[kb] = *reinterpret_cast<const bf16x8_t*>(row + kScaleGroup * rq + 8 * kb);
+  }
+  template <bool kV>
+  __device__ static void load(Tile& x, int u, const ShapedParams& p, size_t off, bool valid,
+                              int lane) {
+    const __amdgpu_buffer_rsrc_t r = bytes_rsrc(p.k + off, valid ? kPackedRecord : 0);
+    x.k[u] = tile_load16(r, 16 * lane);
+    x.ke[u] = __builtin_amdgcn_raw_buffer_load_b8(r, kPackedKExp + lane, 0, kNontemporal);
+    if constexpr (kV) {
+      x.v[u] = tile_load16(r, kPackedV + 16 * lane);
+      x.ve[u] = __builtin_amdgcn_raw_buffer_load_b32(
+          r, kPackedVExp + 16 * (lane >> 4) + 4 * ((lane & 15) >> 2), 0, kNontemporal);
+    }
+  }
+  __device__ static float scale_of(uint32_t exponent) {
+    return __builtin_bit_cast(float, exponent << 23);
+  }
+  // Eight 4-bit numbers times their scale.
+  __device__ static bf16x8_t eight(uint32_t word, float scale) {
+    const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 0);
+    const bf16x2_t b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 1);
+    const bf16x2_t c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 2);
+    const bf16x2_t d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 3);
+    const u32x4_t r = {__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b),
+                       __builtin_bit_cast(uint32_t, c), __builtin_bit_cast(uint32_t, d)};
+    return __builtin_bit_cast(bf16x8_t, r);
+  }
+  __device__ static void scores(const Tile& x, const Q& q, float (&s)[kValues], int lane) {
+    f32x4_t a[kStep];
+#pragma unroll
+    for (int u = 0; u < kStep; ++u) {
+      a[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      const float scale = scale_of(x.ke[u]);
+#pragma unroll
+      for (int kb = 0; kb < 4; ++kb)
+        a[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(eight(x.k[u][kb], scale), q.f[kb], a[u], 0,
+                                                       0, 0);
+    }
+    const bool second = lane & 8;
+#pragma unroll
+    for (int v = 0; v < kValues; ++v) {
+      if constexpr (kTwice)
+        s[v] = second ? a[2 * (v / 4) + 1][v % 4] : a[2 * (v / 4)][v % 4];
+      else
+        s[v] = a[v / 4][v % 4];
+    }
+  }
+  __device__ static int32_t position(int v, const int32_t (&first)[kStep], int lane) {
+    const int32_t t = kTwice ? (lane & 8 ? first[2 * v + 1] : first[2 * v]) : first[v];
+    return t + 4 * (lane >> 4);
+  }
+  // A record may hold anything where no token was written, NaN among it: its
+  // numbers and their exponent are both replaced.
+  __device__ static void hide_value(Tile& x, int u, int i) {
+    x.v[u][i] = 0;
+    x.ve[u] = (x.ve[u] & ~(0xFFu << (8 * i))) | (127u << (8 * i));
+  }
+  __device__ static float head_max(float v) {
+    v = max_over_rows(v);
+    return kTwice ? fmaxf(v, from_xor8(v)) : v;
+  }
+  __device__ static float head_sum(float v) {
+    v = sum_over_rows(v);
+    return kTwice ? v + from_xor8(v) : v;
+  }
+  __device__ static void add_values(f32x4_t (&acc)[8], const Tile& x, const float (&w)[kValues],
+                                    int lane) {
+    const bool second = lane & 8;
+#pragma unroll
+    for (int pair = 0; pair < kStep / 2; ++pair) {
+      // Weights of the two blocks: four tokens of each, two to a register.
+      u32x4_t hi, lo;
+      if constexpr (kTwice) {
+        uint32_t h[2], l[2];
+        split(w + 4 * pair, h, l);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t keep = second ? l[i] : h[i];
+          const uint32_t got = from_xor8(second ? h[i] : l[i]);
+          hi[i] = second ? got : keep;
+          hi[2 + i] = second ? keep : got;
+        }
+      } else {
+        uint32_t h[2], l[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          split(w + 8 * pair + 4 * b, h, l);
+          hi[2 * b] = h[0];
+          hi[2 * b + 1] = h[1];
+          lo[2 * b] = l[0];
+          lo[2 * b + 1] = l[1];
+        }
+      }
+      float scale[2][4];
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          scale[b][i] = scale_of((x.ve[2 * pair + b] >> (8 * i)) & 0xFF);
+      auto product = [&](int m, const u32x4_t& a) {
+        acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a),
+                                                         __builtin_bit_cast(bf16x8_t, hi), acc[m],
+                                                         0, 0, 0);
+        if constexpr (!kTwice)
+          acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a),
+                                                           __builtin_bit_cast(bf16x8_t, lo),
+                                                           acc[m], 0, 0, 0);
+      };
+      // Dims 2j and 2j + 1 of the lane's octet: a pair of dims of each token
+      // becomes a pair of tokens of each dim.
+      auto dims = [&](int m, auto conv) {
+        u32x4_t even, odd;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint32_t t0 = conv(x.v[2 * pair + b][2 * i], scale[b][2 * i]);
+            const uint32_t t1 = conv(x.v[2 * pair + b][2 * i + 1], scale[b][2 * i + 1]);
+            even[2 * b + i] = __builtin_amdgcn_perm(t1, t0, 0x05040100);
+            odd[2 * b + i] = __builtin_amdgcn_perm(t1, t0, 0x07060302);
+          }
+        product(m, even);
+        product(m + 1, odd);
+      };
+      dims(0, [](uint32_t a, float f) { return pair_of<0>(a, f); });
+      dims(2, [](uint32_t a, float f) { return pair_of<1>(a, f); });
+      dims(4, [](uint32_t a, float f) { return pair_of<2>(a, f); });
+      dims(6, [](uint32_t a, float f) { return pair_of<3>(a, f); });
+    }
+  }
+  template <int kByte>
+  __device__ static uint32_t pair_of(uint32_t word, float scale) {
+    return __builtin_bit_cast(uint32_t,
+                              __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, kByte));
+  }
+  // bf16 hi and lo halves of four weights, two to a register.
+  __device__ static void split(const float* w, uint32_t (&hi)[2], uint32_t (&lo)[2]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const bf16x2_t h = {(__bf16)w[2 * i], (__bf16)w[2 * i + 1]};
+      const bf16x2_t l = {(__bf16)(w[2 * i] - (float)h[0]), (__bf16)(w[2 * i + 1] - (float)h[1])};
+      hi[i] = __builtin_bit_cast(uint32_t, h);
+      lo[i] = __builtin_bit_cast(uint32_t, l);
+    }
+  }
+  __device__ static void fold(f32x4_t (&acc)[8]) {
+    if constexpr (kTwice) {
+#pragma unroll
+      for (int m = 0; m < 8; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[m][i] += from_xor8(acc[m][i]);
+    }
+  }
+  // acc[m][i] is dim 8 (4 rq + i) + m.
+  template <class Fn>
+  __device__ static void each_word(const f32x4_t (&acc)[8], int lane, Fn fn) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+        fn(2 * (4 * (lane >> 4) + i) + half,
+           f32x4_t{acc[4 * half][i], acc[4 * half + 1][i], acc[4 * half + 2][i],
+                   acc[4 * half + 3][i]});
+  }
+};
+
+// ------------------------------------------------------------------ a step
+
+// What stays the same over the steps of a (request, kv head) pair.
+template <class C>
+struct Pair {
+  typename C::Q q;
+  Seen seen;
+  const int32_t* row;  // of the block table
+  size_t head_off;     // bytes from a block to this kv head's tile
+  // Distances are counted from the token of this head's largest bias, so that
+  // the biases that matter are small numbers.
+  float slope_log2;
+  int32_t origin;
+};
+
+template <class C>
+__device__ inline Pair<C> make_pair(const ShapedParams& p, int32_t b, int32_t g, const Seen& seen,
+                                    int lane) {
+  Pair<C> pr;
+  pr.seen = seen;
+  pr.row = p.table + (size_t)b * p.mbps;
+  pr.head_off = (size_t)g * C::kHeadBytes;
+  const int h = C::head(lane);
+  const float slope = p.slopes && h < C::G ? p.slopes[g * C::G + h] : 0.f;
+  pr.slope_log2 = slope * 1.4426950408889634f;
+  pr.origin = slope >= 0.f ? seen.L - 1 : seen.first();
+  C::load_q(pr.q, p.q + ((size_t)b * p.hq + g * C::G) * kHeadDim, lane);
+  return pr;
+}
+// The bias of token `origin`, which the scores leave out (natural units): its
+// slope times a distance.
+template <class C>
+__device__ inline float left_out(const ShapedParams& p, int32_t g, int h, const Seen& seen) {
+  if (!p.slopes) return 0.f;
+  const float slope = p.slopes[g * C::G + h];
+  return slope >= 0.f ? 0.f : slope * (float)(seen.first() - (seen.L - 1));
+}
+
+// The physical blocks of step j (virtual blocks kStep j ..), and their first
+// tokens; where there is no block, a token that nobody sees.
+template <class C>
+struct Blocks {
+  int32_t id[C::kStep], first[C::kStep];
+};
+constexpr int32_t kNoToken = 0x7FFFFF00;
+
+template <class C>
+__device__ inline Blocks<C> find_blocks(const Pair<C>& pr, int32_t j) {
+  Blocks<C> r;
+#pragma unroll
+  for (int u = 0; u < C::kStep; ++u) {
+    const int32_t vb = j * C::kStep + u;
+    const int32_t blk = pr.seen.block_of(min(vb, pr.seen.n - 1));
+    r.id[u] = scalar_ints(pr.row)[blk];
+    r.first[u] = vb < pr.seen.n ? blk * kBlock : kNoToken;
+  }
+  return r;
+}
+
+template <class C, bool kV>
+__device__ inline void load_step(const ShapedParams& p, const Pair<C>& pr, const Blocks<C>& at,
+                                 bool valid, typename C::Tile& t, int lane) {
+#pragma unroll
+  for (int u = 0; u < C::kStep; ++u) {
+    const uint32_t id = min((uint32_t)at.id[u], (uint32_t)(p.num_blocks - 1));
+    C::template load<kV>(t, u, p, (size_t)id * (size_t)p.blk_bytes + pr.head_off,
+                         valid && at.first[u] != kNoToken, lane);
+  }
+}
+
+// The step's scores, in base 2 and without the bias of the pair's origin.
+template <class C>
+__device__ inline void shaped_scores(const ShapedParams& p, const Pair<C>& pr,
+                                     const typename C::Tile& t, const Blocks<C>& at, bool all,
+                                     float (&x)[C::kValues], int lane) {
+  C::scores(t, pr.q, x, lane);
+  if (p.cap_log2 != 0.f) {
+#pragma unroll
+    for (int v = 0; v < C::kValues; ++v) x[v] = p.cap_log2 * tanh_score(x[v] * p.cap_in);
+  } else {
+#pragma unroll
+    for (int v = 0; v < C::kValues; ++v) x[v] *= p.scale_log2;
+  }
+  if (p.slopes) {
+#pragma unroll
+    for (int v = 0; v < C::kValues; v += 4) {
+      const int32_t d = C::position(v / 4, at.first, lane) - pr.origin;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[v + i] = fmaf(pr.slope_log2, (float)(d + i), x[v + i]);
+    }
+  }
+  if (!all) {
+#pragma unroll
+    for (int v = 0; v < C::kValues; v += 4) {
+      const int32_t t0 = C::position(v / 4, at.first, lane);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (!pr.seen.sees(t0 + i)) x[v + i] = -INFINITY;
+    }
+  }
+}
+
+// The running softmax of one head (and the sums of its lanes).
+struct Softmax {
+  f32x4_t acc[8];
+  float m;  // maximum so far, the same in all lanes of a head
+  float l;  // this lane's share of the denominator
+  __device__ void init() {
+#pragma unroll
+    for (int mb = 0; mb < 8; ++mb) acc[mb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    m = kLowest;
+    l = 0.f;
+  }
+};
+
+template <class C>
+__device__ inline void attend_step(const ShapedParams& p, const Pair<C>& pr, typename C::Tile& t,
+                                   const Blocks<C>& at, int32_t j, Softmax& st, int lane) {
+  const bool all = pr.seen.sees_all(j * C::kStep, C::kStep);
+  float x[C::kValues];
+  shaped_scores<C>(p, pr, t, at, all, x, lane);
+  if (!all) {
+#pragma unroll
+    for (int u = 0; u < C::kStep; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (!pr.seen.sees(at.first[u] + 4 * (lane >> 4) + i)) C::hide_value(t, u, i);
+  }
+  float mt = x[0];
+#pragma unroll
+  for (int v = 1; v < C::kValues; ++v) mt = fmaxf(mt, x[v]);
+  const float mn = fmaxf(st.m, C::head_max(mt));
+  const float alpha = __builtin_amdgcn_exp2f(st.m - mn);
+  float sum = 0.f;
+#pragma unroll
+  for (int v = 0; v < C::kValues; ++v) {
+    x[v] = __builtin_amdgcn_exp2f(x[v] - mn);
+    sum += x[v];
+  }
+  st.l = fmaf(st.l, alpha, sum);
+  st.m = mn;
+  // Maxima stop growing after a few steps.
+  if (__any(alpha != 1.f)) {
+#pragma unroll
+    for (int mb = 0; mb < 8; ++mb) st.acc[mb] *= alpha;
+  }
+  C::add_values(st.acc, t, x, lane);
+}
+
+// Steps j0, j0 + stride, ... below j1 of a pair, one step's tiles in flight ahead
+// of the one computed and the block ids another step ahead.
+template <class C, bool kV, class Body>
+__device__ inline void each_step(const ShapedParams& p, const Pair<C>& pr, int32_t j0, int32_t j1,
+                                 int32_t stride, int lane, Body body) {
+  if (j0 >= j1) return;
+  typename C::Tile t0, t1;
+  const int32_t last = j1 - 1;
+  Blocks<C> a0 = find_blocks<C>(pr, j0);
+  Blocks<C> a1 = find_blocks<C>(pr, min(j0 + stride, last));
+  load_step<C, kV>(p, pr, a0, true, t0, lane);
+  for (int32_t j = j0;;) {
+    Blocks<C> next = find_blocks<C>(pr, min(j + 2 * stride, last));
+    load_step<C, kV>(p, pr, a1, j + stride < j1, t1, lane);
+    body(t0, a0, j);
+    j += stride;
+    if (j >= j1) break;
+    a0 = next;
+    next = find_blocks<C>(pr, min(j + 2 * stride, last));
+    load_step<C, kV>(p, pr, a0, j + stride < j1, t0, lane);
+    body(t1, a1, j);
+    j += stride;
+    if (j >= j1) break;
+    a1 = next;
+  }
+}
+
+}  // namespace neo

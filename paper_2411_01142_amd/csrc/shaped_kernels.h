@@ -1,0 +1,246 @@
+// Kernels of attention with shaped scores, and of the sums of its weights, over
+// either cache type: a workgroup of eight wavefronts takes a (request, kv head)
+// pair or one of `parts` equal shares of it.
+#pragma once
+
+#include "shaped.h"
+
+namespace neo {
+namespace {
+
+constexpr int kShapedWaves = 8;
+constexpr int kShapedThreads = kWave * kShapedWaves;
+// A share has at least this many steps for every wavefront.
+constexpr int32_t kStepsPerWave = 2;
+
+// Workgroups that share `steps` steps of a pair.
+__device__ inline int32_t shares_of(int32_t steps, int32_t parts) {
+  return min(parts, (steps - 1) / (kShapedWaves * kStepsPerWave) + 1);
+}
+
+struct PairIndex {
+  int32_t s, g, b;
+};
+__device__ inline PairIndex pair_index(const ShapedParams& p) {
+  const int32_t pair = blockIdx.x / p.parts;
+  return {(int32_t)blockIdx.x - pair * p.parts, pair % p.hkv, pair / p.hkv};
+}
+
+template <class C>
+__device__ inline float natural_lse(const ShapedParams& p, int32_t g, int h, const Seen& seen,
+                                    float m, float l) {
+  return (m + __log2f(l)) * kLn2 + left_out<C>(p, g, h, seen);
+}
+
+template <class C>
+__global__ __launch_bounds__(kShapedThreads, 1) void attend_kernel(ShapedParams p) {
+  constexpr int G = C::G;
+  __shared__ float rows[kShapedWaves][G * kHeadDim];  // word c of row h at c ^ h
+  __shared__ float ms[kShapedWaves][G], ls[kShapedWaves][G];
+  __shared__ int32_t arrived;
+  const int lane = threadIdx.x & (kWave - 1);
+  const int wv = uniform(threadIdx.x >> 6);
+  const PairIndex at = pair_index(p);
+  const Seen seen = make_uniform(load_seen(p, at.b));
+  const int32_t row0 = at.b * p.hq + at.g * G;
+  float* out = p.out + (size_t)row0 * kHeadDim;
+  if (seen.n == 0) {
+    if (at.s != 0) return;
+    for (int i = threadIdx.x; i < G * kHeadDim; i += kShapedThreads) out[i] = 0.f;
+    if (p.lse && threadIdx.x < G) p.lse[row0 + threadIdx.x] = -INFINITY;
+    return;
+  }
+  const int32_t steps = (seen.n - 1) / C::kStep + 1;
+  const int32_t shares = shares_of(steps, p.parts);
+  if (at.s >= shares) return;
+  const int32_t j0 = (int32_t)((int64_t)steps * at.s / shares);
+  const int32_t j1 = (int32_t)((int64_t)steps * (at.s + 1) / shares);
+  const int waves = min(kShapedWaves, j1 - j0);  // with steps, the first ones
+
+  const Pair<C> pr = make_pair<C>(p, at.b, at.g, seen, lane);
+  Softmax st;
+  st.init();
+  each_step<C, true>(p, pr, j0 + wv, j1, kShapedWaves, lane,
+                     [&](typename C::Tile& t, const Blocks<C>& blocks, int32_t j) {
+                       attend_step<C>(p, pr, t, blocks, j, st, lane);
+                     });
+  if (wv < waves) {
+    C::fold(st.acc);
+    const float l = C::head_sum(st.l);
+    const int h = lane & 15;
+    if (h < G) {
+      C::each_word(st.acc, lane, [&](int c, f32x4_t v) {
+        *reinterpret_cast<f32x4_t*>(&rows[wv][h * kHeadDim + 4 * (c ^ h)]) = v;
+      });
+      if (lane < 16) {
+        ms[wv][h] = st.m;
+        ls[wv][h] = l;
+      }
+    }
+  }
+  __syncthreads();
+  const int32_t pair = at.b * p.hkv + at.g;
+  const size_t slot = (size_t)pair * p.parts + at.s;
+  for (int h = wv; h < G; h += kShapedWaves) {
+    float m = kLowest, l = 0.f, x = 0.f, y = 0.f;
+    for (int w = 0; w < waves; ++w) m = fmaxf(m, ms[w][h]);
+    for (int w = 0; w < waves; ++w) {
+      const float e = __builtin_amdgcn_exp2f(ms[w][h] - m);
+      const float2 v =
+          *reinterpret_cast<const float2*>(&rows[w][h * kHeadDim + ((2 * lane) ^ (4 * h))]);
+      l = fmaf(e, ls[w][h], l);
+      x = fmaf(e, v.x, x);
+      y = fmaf(e, v.y, y);
+    }
+    if (shares == 1) {
+      const float inv = 1.f / l;
+      *reinterpret_cast<float2*>(out + h * kHeadDim + 2 * lane) = float2{x * inv, y * inv};
+      if (p.lse && lane == 0) p.lse[row0 + h] = natural_lse<C>(p, at.g, h, seen, m, l);
+    } else {
+      store_coherent2(p.part_o + (slot * G + h) * kHeadDim + 2 * lane, x, y);
+      if (lane == 0) store_coherent2(p.part_ml + (slot * G + h) * 2, m, l);
+    }
+  }
+  if (shares == 1) return;
+  // Every wavefront's stores are complete before the workgroup is counted; the
+  // last workgroup of the pair merges it and leaves the counter at zero.
+  wait_all_memory();
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const int32_t old =
+        __hip_atomic_fetch_add(p.counters + pair, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (old == shares - 1)
+      __hip_atomic_store(p.counters + pair, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    arrived = old;
+  }
+  __syncthreads();
+  if (arrived != shares - 1) return;
+  const size_t slot0 = (size_t)pair * p.parts;
+  for (int h = wv; h < G; h += kShapedWaves) {
+    float m = kLowest, l = 0.f, x = 0.f, y = 0.f;
+    for (int32_t base = 0; base < shares; base += kWave) {
+      const int32_t cnt = min(kWave, shares - base);
+      const size_t mine = slot0 + base + min(lane, cnt - 1);
+      const float2 ml = load_coherent2(p.part_ml + (mine * G + h) * 2);
+      const float mc = fmaxf(m, wave_max_f32(ml.x));
+      const float w = lane < cnt ? __builtin_amdgcn_exp2f(ml.x - mc) : 0.f;
+      const float scale = __builtin_amdgcn_exp2f(m - mc);  // 0 on the first round
+      m = mc;
+      l = l * scale + wave_sum_f32(lane < cnt ? w * ml.y : 0.f);
+      x *= scale;
+      y *= scale;
+      constexpr int kBatch = 16;
+      for (int32_t i0 = 0; i0 < cnt; i0 += kBatch) {
+        float2 v[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u)
+          v[u] = load_coherent2(p.part_o +
+                                ((slot0 + base + min(i0 + u, cnt - 1)) * G + h) * kHeadDim +
+                                2 * lane);
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+          if (i0 + u >= cnt) break;
+          const float wi = __builtin_bit_cast(
+              float, __builtin_amdgcn_readlane(__builtin_bit_cast(int32_t, w), i0 + u));
+          x = fmaf(wi, v[u].x, x);
+          y = fmaf(wi, v[u].y, y);
+        }
+      }
+    }
+    const float inv = 1.f / l;
+    *reinterpret_cast<float2*>(out + h * kHeadDim + 2 * lane) = float2{x * inv, y * inv};
+    if (p.lse && lane == 0) p.lse[row0 + h] = natural_lse<C>(p, at.g, h, seen, m, l);
+  }
+}
+
+// Sum over the heads of a token's weights: lanes of the 16-lane row (or of each
+// half of it, where the columns hold the heads twice).
+template <int kCtrl>
+__device__ inline float dpp_f32(float v) {
+  return __builtin_bit_cast(
+      float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), kCtrl, 0xF, 0xF, true));
+}
+template <bool kHalves>
+__device__ inline float sum_over_columns(float v) {
+  constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kHalfMirror = 0x141;
+  v += dpp_f32<kXor1>(v);
+  v += dpp_f32<kXor2>(v);
+  v += dpp_f32<kHalfMirror>(v);
+  if constexpr (!kHalves) v += from_xor8(v);
+  return v;
+}
+
+// sums_out[b][g][t] = sums[b][g][t] + sum over the group's heads of exp(x_t - lse),
+// for the tokens that the request sees. Reads K alone.
+template <class C>
+__global__ __launch_bounds__(kShapedThreads, 1) void weights_kernel(ShapedParams p) {
+  constexpr bool kHalves = C::kValues == 8;
+  const int lane = threadIdx.x & (kWave - 1);
+  const int wv = uniform(threadIdx.x >> 6);
+  const PairIndex at = pair_index(p);
+  const Seen seen = make_uniform(load_seen(p, at.b));
+  if (seen.n == 0) return;
+  const int32_t steps = (seen.n - 1) / C::kStep + 1;
+  const int32_t shares = shares_of(steps, p.parts);
+  if (at.s >= shares) return;
+  const int32_t j0 = (int32_t)((int64_t)steps * at.s / shares);
+  const int32_t j1 = (int32_t)((int64_t)steps * (at.s + 1) / shares);
+  const Pair<C> pr = make_pair<C>(p, at.b, at.g, seen, lane);
+  const int h = C::head(lane), col = lane & 15;
+  const bool real = h < C::G;
+  // lse in base 2, without the bias of the pair's origin; one rounding, since
+  // both may be large and nearly the same.
+  float lse = 0.f;
+  if (real) {
+    const float slope = p.slopes ? p.slopes[at.g * C::G + h] : 0.f;
+    const float d = slope < 0.f ? (float)(seen.first() - (seen.L - 1)) : 0.f;
+    lse = fmaf(-slope, d, p.lse_in[at.b * p.hq + at.g * C::G + h]) * 1.4426950408889634f;
+  }
+  const size_t row = ((size_t)at.b * p.hkv + at.g) * (size_t)p.sums_stride;
+  each_step<C, false>(
+      p, pr, j0 + wv, j1, kShapedWaves, lane,
+      [&](typename C::Tile& t, const Blocks<C>& blocks, int32_t j) {
+        float x[C::kValues];
+        const bool all = seen.sees_all(j * C::kStep, C::kStep);
+        shaped_scores<C>(p, pr, t, blocks, all, x, lane);
+#pragma unroll
+        for (int v = 0; v < C::kValues; v += 4) {
+          const int32_t t0 = C::position(v / 4, blocks.first, lane);
+          float w[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            w[i] = sum_over_columns<kHalves>(real ? __builtin_amdgcn_exp2f(x[v + i] - lse) : 0.f);
+          // Columns 0-3 (and 8-11) write a token each.
+          const int i = col & 3;
+          const float mine = i < 2 ? (i == 0 ? w[0] : w[1]) : (i == 2 ? w[2] : w[3]);
+          const bool writes = kHalves ? (col & 4) == 0 : col < 4;
+          if (writes && seen.sees(t0 + i)) p.sums_out[row + t0 + i] = p.sums[row + t0 + i] + mine;
+        }
+      });
+}
+
+}  // namespace
+
+template <template <int> class Cache, int G>
+hipError_t launch_shaped_g(const ShapedParams& p, bool weights, hipStream_t stream) {
+  const unsigned grid = (unsigned)((int64_t)p.batch * p.hkv * p.parts);
+  if (weights)
+    weights_kernel<Cache<G>><<<grid, kShapedThreads, 0, stream>>>(p);
+  else
+    attend_kernel<Cache<G>><<<grid, kShapedThreads, 0, stream>>>(p);
+  return hipGetLastError();
+}
+
+template <template <int> class Cache>
+hipError_t launch_shaped(const ShapedParams& p, int32_t group, bool weights, hipStream_t stream) {
+  switch (group) {
+    case 1: return launch_shaped_g<Cache, 1>(p, weights, stream);
+    case 2: return launch_shaped_g<Cache, 2>(p, weights, stream);
+    case 4: return launch_shaped_g<Cache, 4>(p, weights, stream);
+    case 8: return launch_shaped_g<Cache, 8>(p, weights, stream);
+    case 16: return launch_shaped_g<Cache, 16>(p, weights, stream);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+}  // namespace neo
