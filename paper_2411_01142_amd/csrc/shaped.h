@@ -277,8 +277,12 @@ struct PackedCache {
     }
   }
   __device__ static int32_t position(int v, const int32_t (&first)[kStep], int lane) {
-    const int32_t t = kTwice ? (lane & 8 ? first[2 * v + 1] : first[2 * v]) : first[v];
-    return t + 4 * (lane >> 4);
+    if constexpr (kTwice) {
+      const int32_t a = first[2 * v], b = first[2 * v + 1];
+      return (lane & 8 ? b : a) + 4 * (lane >> 4);
+    } else {
+      return first[v] + 4 * (lane >> 4);
+    }
   }
   // A record may hold anything where no token was written, NaN among it: its
   // numbers and their exponent are both replaced.
