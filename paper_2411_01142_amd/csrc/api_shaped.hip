@@ -105,6 +105,10 @@ int32_t parts_of(int32_t batch, int32_t hkv, int32_t mbps, int32_t blocks_per_st
   return (int32_t)std::min<int64_t>(most, std::max<int64_t>(1, cus / pairs));
 }
 
+// A call in slices has a workgroup per compute unit; no more than the workspace has
+// slots for (two each) and slices may be numbered.
+constexpr int32_t kMostSliceGroups = NEO_MAX_SLICES / 16;
+
 struct Cache {
   const void* k;
   const void* v;   // null: packed
@@ -168,6 +172,8 @@ neo_status attend(const void* q, const Cache& cache, bool packed, const int32_t*
   // compute unit, where the workspace has NEO_MAX_SLICES counters and as many
   // slots of rows, maxima and denominators.)
   p.parts = parts_of(batch, hkv, mbps, packed ? 4 : 1, std::min(cus, NEO_MAX_SLICES));
+  p.xcd8 = xcds == 8;
+  p.slices = (int64_t)batch * hkv > cus ? std::min(cus, kMostSliceGroups) : 0;
   hipStream_t s = static_cast<hipStream_t>(stream);
   return launched(packed ? launch_shaped_packed(p, group, false, s)
                          : launch_shaped_bf16(p, group, false, s),

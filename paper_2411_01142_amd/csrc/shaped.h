@@ -34,6 +34,8 @@ struct ShapedParams {
   int64_t sums_stride;
   int32_t batch, hq, hkv, mbps, num_blocks;
   int32_t parts;            // workgroups of a (request, kv head) pair, at most
+  int32_t xcd8;             // the device has eight XCDs
+  int32_t slices;           // workgroups of a call in slices, 0: in pairs
   float scale_log2;         // scale * log2(e)
   float cap_in, cap_log2;   // scale / cap and cap * log2(e); cap_log2 0: no cap
 };
@@ -63,18 +65,6 @@ __device__ inline Seen make_seen(int32_t len, int32_t start, int32_t prefix, int
   v.n = v.pb + nb - v.f;
   return v;
 }
-__device__ inline Seen load_seen(const ShapedParams& p, int32_t b) {
-  return make_seen(p.lens[b], p.starts ? p.starts[b] : 0, p.prefix ? p.prefix[b] : 0, p.mbps);
-}
-__device__ inline Seen make_uniform(Seen v) {
-  v.L = uniform(v.L);
-  v.p = uniform(v.p);
-  v.s = uniform(v.s);
-  v.pb = uniform(v.pb);
-  v.f = uniform(v.f);
-  v.n = uniform(v.n);
-  return v;
-}
 
 // Wave-uniform reads of the block table through the scalar cache: they neither
 // occupy vector registers nor stand in the queue of the tile loads, whose
@@ -82,12 +72,21 @@ __device__ inline Seen make_uniform(Seen v) {
 typedef const __attribute__((address_space(4))) int32_t* ScalarInts;
 __device__ inline ScalarInts scalar_ints(const int32_t* p) { return (ScalarInts)(uintptr_t)p; }
 
-__device__ inline __amdgpu_buffer_rsrc_t bytes_rsrc(const uint8_t* base, int32_t bytes) {
-  const uint64_t a = reinterpret_cast<uint64_t>(base);
-  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)a);
-  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32));
-  void* u = reinterpret_cast<void*>(((uint64_t)hi << 32) | lo);
-  return __builtin_amdgcn_make_buffer_rsrc(u, (short)0, uniform(bytes), kBufferWord3);
+// Of a request that all lanes agree on.
+__device__ inline Seen load_seen(const ShapedParams& p, int32_t b) {
+  return make_seen(scalar_ints(p.lens)[b], p.starts ? scalar_ints(p.starts)[b] : 0,
+                   p.prefix ? scalar_ints(p.prefix)[b] : 0, p.mbps);
+}
+// Of a request of each lane's own.
+__device__ inline Seen lane_seen(const ShapedParams& p, int32_t b) {
+  return make_seen(p.lens[b], p.starts ? p.starts[b] : 0, p.prefix ? p.prefix[b] : 0, p.mbps);
+}
+
+// A tile's words, from an address that all lanes agree on and an offset of each lane's.
+// Every word is read once: nontemporal loads keep it from displacing what is used again.
+template <class T>
+__device__ inline T stream_load(const uint8_t* base, uint32_t off) {
+  return __builtin_nontemporal_load(reinterpret_cast<const T*>(base + off));
 }
 
 // Lane l's value from lane l ^ 8 (a rotation of each 16-lane row by eight).
@@ -126,6 +125,9 @@ struct Bf16Cache {
   static constexpr int kStep = 1;
   static constexpr int kValues = 4;
   static constexpr int kHeadBytes = kTileBytes;
+  static constexpr int kSliceWaves = 4;      // slices of a workgroup (one per compute unit)
+  // s_waitcnt vmcnt(16): all but the loads of a step (12) and of query rows (4).
+  static constexpr int kWaitOneStep = 0x4F70;
   struct Tile {
     bf16x8_t k[4];
     s16x4_t v[8];
@@ -141,19 +143,19 @@ struct Bf16Cache {
     for (int kb = 0; kb < 4; ++kb)
       q.f[kb] = *reinterpret_cast<const bf16x8_t*>(row + kPiece * (4 * kb + rq));
   }
-  template <bool kV>
-  __device__ static void load(Tile& x, int, const ShapedParams& p, size_t off, bool valid,
-                              int lane) {
-    const int col = lane & 15, rq = lane >> 4;
-    const __amdgpu_buffer_rsrc_t rk = bytes_rsrc(p.k + off, valid ? kTileBytes : 0);
+  template <bool kK, bool kV>
+  __device__ static void load(Tile& x, int, const ShapedParams& p, size_t off, int lane) {
+    if constexpr (kK) {
 #pragma unroll
-    for (int kb = 0; kb < 4; ++kb)
-      x.k[kb] = __builtin_bit_cast(bf16x8_t, tile_load16(rk, 2 * kPiece * (kWave * kb + lane)));
+      for (int kb = 0; kb < 4; ++kb)
+        x.k[kb] = stream_load<bf16x8_t>(p.k + off + 2 * kPiece * kWave * kb, 2 * kPiece * lane);
+    }
     if constexpr (kV) {
-      const __amdgpu_buffer_rsrc_t rv = bytes_rsrc(p.v + off, valid ? kTileBytes : 0);
+      const int col = lane & 15, rq = lane >> 4;
 #pragma unroll
       for (int mb = 0; mb < 8; ++mb)
-        x.v[mb] = tile_load8(rv, 2 * ((16 * mb + col) * kBlock + 4 * rq));
+        x.v[mb] = stream_load<s16x4_t>(p.v + off + 2 * 16 * kBlock * mb,
+                                       2 * (col * kBlock + 4 * rq));
     }
   }
   __device__ static void scores(const Tile& x, const Q& q, float (&s)[kValues], int) {
@@ -174,21 +176,26 @@ struct Bf16Cache {
   }
   __device__ static float head_max(float v) { return max_over_rows(v); }
   __device__ static float head_sum(float v) { return sum_over_rows(v); }
-  // Weights enter the product as bf16 hi + lo halves, about 16 bits of each.
+  // Weights enter the product as three bf16 numbers each, of 8 bits more and more: with
+  // two, a result is off by 1 to 2.5e-6 of itself, with three by the fp32 sums' roundings.
   __device__ static void add_values(f32x4_t (&acc)[8], const Tile& x, const float (&w)[kValues],
                                     int) {
-    s16x4_t hi, lo;
+    s16x4_t part[3];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const __bf16 h = (__bf16)w[i];
-      hi[i] = __builtin_bit_cast(short, h);
-      lo[i] = __builtin_bit_cast(short, (__bf16)(w[i] - (float)h));
+      float rest = w[i];
+#pragma unroll
+      for (int k = 0; k < 3; ++k) {
+        const __bf16 h = (__bf16)rest;
+        part[k][i] = __builtin_bit_cast(short, h);
+        rest -= (float)h;
+      }
     }
 #pragma unroll
-    for (int mb = 0; mb < 8; ++mb) {
-      acc[mb] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(x.v[mb], hi, acc[mb], 0, 0, 0);
-      acc[mb] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(x.v[mb], lo, acc[mb], 0, 0, 0);
-    }
+    for (int mb = 0; mb < 8; ++mb)
+#pragma unroll
+      for (int k = 0; k < 3; ++k)
+        acc[mb] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(x.v[mb], part[k], acc[mb], 0, 0, 0);
   }
   __device__ static void fold(f32x4_t (&)[8]) {}
   // Word c (dims 4c .. 4c + 3) of this lane's head, for its eight words.
@@ -203,12 +210,13 @@ struct Bf16Cache {
 // that the running maximum, the rescaling and the addresses are paid once for 64
 // tokens. Records become bf16 in registers, a pair of values an instruction.
 //
-// With up to eight heads a matrix product's 16 columns hold them twice. Of the
-// scores of two blocks, lanes of columns 0-7 keep the first block's and those of
-// columns 8-15 the second's, so that half as many are left to each lane; and in
-// the second product columns 0-7 carry the weights' bf16 hi halves and 8-15 the
-// lo halves, so that one product does the work of two. The lanes exchange the
-// halves that the other needs with a rotation by eight.
+// With up to eight heads a matrix product's 16 columns hold them twice. Of the scores
+// of two blocks, lanes of columns 0-7 keep the first block's and those of columns 8-15
+// the second's, so that half as many are left to each lane. The weights are sums of three
+// bf16 numbers, as over bf16 caches: in one product columns 0-7 carry the first ones and
+// 8-15 the second ones of both blocks (the lanes exchange what the other needs with a
+// rotation by eight), in another the third ones, of the first block in columns 0-7 and of
+// the second in 8-15, zeros beside them; the two halves of the sums are added in the end.
 template <int G_>
 struct PackedCache {
   static constexpr int G = G_;
@@ -216,6 +224,8 @@ struct PackedCache {
   static constexpr bool kTwice = G <= 8;
   static constexpr int kValues = kTwice ? 8 : 16;
   static constexpr int kHeadBytes = kPackedRecord;
+  static constexpr int kSliceWaves = 8;
+  static constexpr int kWaitOneStep = 0x4F74;  // vmcnt(20): 16 and 4
   struct Tile {
     u32x4_t k[kStep], v[kStep];
     uint32_t ke[kStep], ve[kStep];  // exponent bytes: of the K run, of four V tokens
@@ -231,16 +241,17 @@ struct PackedCache {
     for (int kb = 0; kb < 4; ++kb)
       q.f[kb] = *reinterpret_cast<const bf16x8_t*>(row + kScaleGroup * rq + 8 * kb);
   }
-  template <bool kV>
-  __device__ static void load(Tile& x, int u, const ShapedParams& p, size_t off, bool valid,
-                              int lane) {
-    const __amdgpu_buffer_rsrc_t r = bytes_rsrc(p.k + off, valid ? kPackedRecord : 0);
-    x.k[u] = tile_load16(r, 16 * lane);
-    x.ke[u] = __builtin_amdgcn_raw_buffer_load_b8(r, kPackedKExp + lane, 0, kNontemporal);
+  template <bool kK, bool kV>
+  __device__ static void load(Tile& x, int u, const ShapedParams& p, size_t off, int lane) {
+    const uint8_t* rec = p.k + off;
+    if constexpr (kK) {
+      x.k[u] = stream_load<u32x4_t>(rec, 16 * lane);
+      x.ke[u] = stream_load<uint8_t>(rec + kPackedKExp, lane);
+    }
     if constexpr (kV) {
-      x.v[u] = tile_load16(r, kPackedV + 16 * lane);
-      x.ve[u] = __builtin_amdgcn_raw_buffer_load_b32(
-          r, kPackedVExp + 16 * (lane >> 4) + 4 * ((lane & 15) >> 2), 0, kNontemporal);
+      x.v[u] = stream_load<u32x4_t>(rec + kPackedV, 16 * lane);
+      x.ve[u] =
+          stream_load<uint32_t>(rec + kPackedVExp, 16 * (lane >> 4) + 4 * ((lane & 15) >> 2));
     }
   }
   __device__ static float scale_of(uint32_t exponent) {
@@ -303,27 +314,30 @@ struct PackedCache {
     const bool second = lane & 8;
 #pragma unroll
     for (int pair = 0; pair < kStep / 2; ++pair) {
-      // Weights of the two blocks: four tokens of each, two to a register.
-      u32x4_t hi, lo;
+      // Weights of the two blocks: four tokens of each, two to a register, in three parts.
+      u32x4_t part[3];
       if constexpr (kTwice) {
-        uint32_t h[2], l[2];
-        split(w + 4 * pair, h, l);
+        uint32_t q[3][2];
+        split(w + 4 * pair, q);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const uint32_t keep = second ? l[i] : h[i];
-          const uint32_t got = from_xor8(second ? h[i] : l[i]);
-          hi[i] = second ? got : keep;
-          hi[2 + i] = second ? keep : got;
+          const uint32_t keep = second ? q[1][i] : q[0][i];
+          const uint32_t got = from_xor8(second ? q[0][i] : q[1][i]);
+          part[0][i] = second ? got : keep;
+          part[0][2 + i] = second ? keep : got;
+          part[1][i] = second ? 0 : q[2][i];
+          part[1][2 + i] = second ? q[2][i] : 0;
         }
       } else {
-        uint32_t h[2], l[2];
+        uint32_t q[3][2];
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-          split(w + 8 * pair + 4 * b, h, l);
-          hi[2 * b] = h[0];
-          hi[2 * b + 1] = h[1];
-          lo[2 * b] = l[0];
-          lo[2 * b + 1] = l[1];
+          split(w + 8 * pair + 4 * b, q);
+#pragma unroll
+          for (int k = 0; k < 3; ++k) {
+            part[k][2 * b] = q[k][0];
+            part[k][2 * b + 1] = q[k][1];
+          }
         }
       }
       float scale[2][4];
@@ -333,12 +347,10 @@ struct PackedCache {
         for (int i = 0; i < 4; ++i)
           scale[b][i] = scale_of((x.ve[2 * pair + b] >> (8 * i)) & 0xFF);
       auto product = [&](int m, const u32x4_t& a) {
-        acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a),
-                                                         __builtin_bit_cast(bf16x8_t, hi), acc[m],
-                                                         0, 0, 0);
-        if constexpr (!kTwice)
+#pragma unroll
+        for (int k = 0; k < (kTwice ? 2 : 3); ++k)
           acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a),
-                                                           __builtin_bit_cast(bf16x8_t, lo),
+                                                           __builtin_bit_cast(bf16x8_t, part[k]),
                                                            acc[m], 0, 0, 0);
       };
       // Dims 2j and 2j + 1 of the lane's octet: a pair of dims of each token
@@ -368,14 +380,18 @@ struct PackedCache {
     return __builtin_bit_cast(uint32_t,
                               __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, kByte));
   }
-  // bf16 hi and lo halves of four weights, two to a register.
-  __device__ static void split(const float* w, uint32_t (&hi)[2], uint32_t (&lo)[2]) {
+  // Four weights as sums of three bf16 numbers, two to a register.
+  __device__ static void split(const float* w, uint32_t (&parts)[3][2]) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const bf16x2_t h = {(__bf16)w[2 * i], (__bf16)w[2 * i + 1]};
-      const bf16x2_t l = {(__bf16)(w[2 * i] - (float)h[0]), (__bf16)(w[2 * i + 1] - (float)h[1])};
-      hi[i] = __builtin_bit_cast(uint32_t, h);
-      lo[i] = __builtin_bit_cast(uint32_t, l);
+      float a = w[2 * i], b = w[2 * i + 1];
+#pragma unroll
+      for (int k = 0; k < 3; ++k) {
+        const bf16x2_t h = {(__bf16)a, (__bf16)b};
+        parts[k][i] = __builtin_bit_cast(uint32_t, h);
+        a -= (float)h[0];
+        b -= (float)h[1];
+      }
     }
   }
   __device__ static void fold(f32x4_t (&acc)[8]) {
@@ -401,13 +417,15 @@ struct PackedCache {
 
 // ------------------------------------------------------------------ a step
 
-// What stays the same over the steps of a (request, kv head) pair.
+// A request and kv head with what the request sees; the same in all lanes.
+struct Place {
+  int32_t b, g;
+  Seen seen;
+};
+// The pair's query rows and biases, as a lane holds them.
 template <class C>
 struct Pair {
   typename C::Q q;
-  Seen seen;
-  const int32_t* row;  // of the block table
-  size_t head_off;     // bytes from a block to this kv head's tile
   // Distances are counted from the token of this head's largest bias, so that
   // the biases that matter are small numbers.
   float slope_log2;
@@ -415,17 +433,17 @@ struct Pair {
 };
 
 template <class C>
-__device__ inline Pair<C> make_pair(const ShapedParams& p, int32_t b, int32_t g, const Seen& seen,
-                                    int lane) {
-  Pair<C> pr;
-  pr.seen = seen;
-  pr.row = p.table + (size_t)b * p.mbps;
-  pr.head_off = (size_t)g * C::kHeadBytes;
+__device__ inline void set_bias(const ShapedParams& p, const Place& at, Pair<C>& pr, int lane) {
   const int h = C::head(lane);
-  const float slope = p.slopes && h < C::G ? p.slopes[g * C::G + h] : 0.f;
+  const float slope = p.slopes && h < C::G ? p.slopes[at.g * C::G + h] : 0.f;
   pr.slope_log2 = slope * 1.4426950408889634f;
-  pr.origin = slope >= 0.f ? seen.L - 1 : seen.first();
-  C::load_q(pr.q, p.q + ((size_t)b * p.hq + g * C::G) * kHeadDim, lane);
+  pr.origin = slope >= 0.f ? at.seen.L - 1 : at.seen.first();
+}
+template <class C>
+__device__ inline Pair<C> make_pair(const ShapedParams& p, const Place& at, int lane) {
+  Pair<C> pr;
+  set_bias<C>(p, at, pr, lane);
+  C::load_q(pr.q, p.q + ((size_t)at.b * p.hq + at.g * C::G) * kHeadDim, lane);
   return pr;
 }
 // The bias of token `origin`, which the scores leave out (natural units): its
@@ -437,44 +455,57 @@ __device__ inline float left_out(const ShapedParams& p, int32_t g, int h, const 
   return slope >= 0.f ? 0.f : slope * (float)(seen.first() - (seen.L - 1));
 }
 
-// The physical blocks of step j (virtual blocks kStep j ..), and their first
-// tokens; where there is no block, a token that nobody sees.
+// The physical blocks of step j: of virtual blocks kStep j .., and the last one again
+// where there are no more (its tokens count for nothing there).
 template <class C>
 struct Blocks {
-  int32_t id[C::kStep], first[C::kStep];
+  int32_t id[C::kStep];
 };
-constexpr int32_t kNoToken = 0x7FFFFF00;
-
 template <class C>
-__device__ inline Blocks<C> find_blocks(const Pair<C>& pr, int32_t j) {
+__device__ inline Blocks<C> find_blocks(const ShapedParams& p, const Place& at, int32_t j) {
   Blocks<C> r;
+  const ScalarInts row = scalar_ints(p.table) + (size_t)at.b * p.mbps;
+  const Seen& seen = at.seen;
+  const int32_t v0 = j * C::kStep;
+  if (v0 + C::kStep <= seen.n && (v0 >= seen.pb || v0 + C::kStep <= seen.pb)) {
+    const ScalarInts ids = row + seen.block_of(v0);  // a run of the table
 #pragma unroll
-  for (int u = 0; u < C::kStep; ++u) {
-    const int32_t vb = j * C::kStep + u;
-    const int32_t blk = pr.seen.block_of(min(vb, pr.seen.n - 1));
-    r.id[u] = scalar_ints(pr.row)[blk];
-    r.first[u] = vb < pr.seen.n ? blk * kBlock : kNoToken;
+    for (int u = 0; u < C::kStep; ++u) r.id[u] = ids[u];
+  } else {
+#pragma unroll
+    for (int u = 0; u < C::kStep; ++u) r.id[u] = row[seen.block_of(min(v0 + u, seen.n - 1))];
   }
   return r;
 }
-
-template <class C, bool kV>
-__device__ inline void load_step(const ShapedParams& p, const Pair<C>& pr, const Blocks<C>& at,
-                                 bool valid, typename C::Tile& t, int lane) {
+// First tokens of the step's blocks; where there is no block, a token that nobody sees.
+constexpr int32_t kNoToken = 0x7FFFFF00;
+template <class C>
+__device__ inline void first_tokens(const Seen& seen, int32_t j, int32_t (&first)[C::kStep]) {
 #pragma unroll
   for (int u = 0; u < C::kStep; ++u) {
-    const uint32_t id = min((uint32_t)at.id[u], (uint32_t)(p.num_blocks - 1));
-    C::template load<kV>(t, u, p, (size_t)id * (size_t)p.blk_bytes + pr.head_off,
-                         valid && at.first[u] != kNoToken, lane);
+    const int32_t v = j * C::kStep + u;
+    first[u] = v < seen.n ? seen.block_of(v) * kBlock : kNoToken;
   }
 }
 
-// The step's scores, in base 2 and without the bias of the pair's origin.
+template <class C, bool kK, bool kV>
+__device__ inline void load_step(const ShapedParams& p, const Place& at, const Blocks<C>& blocks,
+                                 typename C::Tile& t, int lane) {
+#pragma unroll
+  for (int u = 0; u < C::kStep; ++u) {
+    const uint32_t id = min((uint32_t)blocks.id[u], (uint32_t)(p.num_blocks - 1));
+    C::template load<kK, kV>(t, u, p,
+                             (size_t)id * (size_t)p.blk_bytes + (size_t)(at.g * C::kHeadBytes),
+                             lane);
+  }
+}
+
+// A step's products q.k become its scores, in base 2 and without the bias of the pair's
+// origin.
 template <class C>
-__device__ inline void shaped_scores(const ShapedParams& p, const Pair<C>& pr,
-                                     const typename C::Tile& t, const Blocks<C>& at, bool all,
-                                     float (&x)[C::kValues], int lane) {
-  C::scores(t, pr.q, x, lane);
+__device__ inline void shape_scores(const ShapedParams& p, const Seen& seen, const Pair<C>& pr,
+                                    const int32_t (&first)[C::kStep], bool all,
+                                    float (&x)[C::kValues], int lane) {
   if (p.cap_log2 != 0.f) {
 #pragma unroll
     for (int v = 0; v < C::kValues; ++v) x[v] = p.cap_log2 * tanh_score(x[v] * p.cap_in);
@@ -485,7 +516,7 @@ __device__ inline void shaped_scores(const ShapedParams& p, const Pair<C>& pr,
   if (p.slopes) {
 #pragma unroll
     for (int v = 0; v < C::kValues; v += 4) {
-      const int32_t d = C::position(v / 4, at.first, lane) - pr.origin;
+      const int32_t d = C::position(v / 4, first, lane) - pr.origin;
 #pragma unroll
       for (int i = 0; i < 4; ++i) x[v + i] = fmaf(pr.slope_log2, (float)(d + i), x[v + i]);
     }
@@ -493,10 +524,10 @@ __device__ inline void shaped_scores(const ShapedParams& p, const Pair<C>& pr,
   if (!all) {
 #pragma unroll
     for (int v = 0; v < C::kValues; v += 4) {
-      const int32_t t0 = C::position(v / 4, at.first, lane);
+      const int32_t t0 = C::position(v / 4, first, lane);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (!pr.seen.sees(t0 + i)) x[v + i] = -INFINITY;
+        if (!seen.sees(t0 + i)) x[v + i] = -INFINITY;
     }
   }
 }
@@ -514,18 +545,21 @@ struct Softmax {
   }
 };
 
+// A step's products x into the running softmax, with its values.
 template <class C>
-__device__ inline void attend_step(const ShapedParams& p, const Pair<C>& pr, typename C::Tile& t,
-                                   const Blocks<C>& at, int32_t j, Softmax& st, int lane) {
-  const bool all = pr.seen.sees_all(j * C::kStep, C::kStep);
-  float x[C::kValues];
-  shaped_scores<C>(p, pr, t, at, all, x, lane);
+__device__ inline void attend_scores(const ShapedParams& p, const Seen& seen, const Pair<C>& pr,
+                                     typename C::Tile& t, int32_t j, float (&x)[C::kValues],
+                                     Softmax& st, int lane) {
+  const bool all = seen.sees_all(j * C::kStep, C::kStep);
+  int32_t first[C::kStep];
+  first_tokens<C>(seen, j, first);
+  shape_scores<C>(p, seen, pr, first, all, x, lane);
   if (!all) {
 #pragma unroll
     for (int u = 0; u < C::kStep; ++u)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (!pr.seen.sees(at.first[u] + 4 * (lane >> 4) + i)) C::hide_value(t, u, i);
+        if (!seen.sees(first[u] + 4 * (lane >> 4) + i)) C::hide_value(t, u, i);
   }
   float mt = x[0];
 #pragma unroll
@@ -547,31 +581,37 @@ __device__ inline void attend_step(const ShapedParams& p, const Pair<C>& pr, typ
   }
   C::add_values(st.acc, t, x, lane);
 }
+template <class C>
+__device__ inline void attend_step(const ShapedParams& p, const Seen& seen, const Pair<C>& pr,
+                                   typename C::Tile& t, int32_t j, Softmax& st, int lane) {
+  float x[C::kValues];
+  C::scores(t, pr.q, x, lane);
+  attend_scores<C>(p, seen, pr, t, j, x, st, lane);
+}
 
 // Steps j0, j0 + stride, ... below j1 of a pair, one step's tiles in flight ahead
 // of the one computed and the block ids another step ahead.
 template <class C, bool kV, class Body>
-__device__ inline void each_step(const ShapedParams& p, const Pair<C>& pr, int32_t j0, int32_t j1,
+__device__ inline void each_step(const ShapedParams& p, const Place& pl, int32_t j0, int32_t j1,
                                  int32_t stride, int lane, Body body) {
   if (j0 >= j1) return;
   typename C::Tile t0, t1;
+  load_step<C, true, kV>(p, pl, find_blocks<C>(p, pl, j0), t0, lane);
+  if (j0 + stride >= j1) return body(t0, j0);
+  // (The last step stands outside of the loop, so that every step in it requests as much.)
   const int32_t last = j1 - 1;
-  Blocks<C> a0 = find_blocks<C>(pr, j0);
-  Blocks<C> a1 = find_blocks<C>(pr, min(j0 + stride, last));
-  load_step<C, kV>(p, pr, a0, true, t0, lane);
+  Blocks<C> ids = find_blocks<C>(p, pl, j0 + stride);
   for (int32_t j = j0;;) {
-    Blocks<C> next = find_blocks<C>(pr, min(j + 2 * stride, last));
-    load_step<C, kV>(p, pr, a1, j + stride < j1, t1, lane);
-    body(t0, a0, j);
+    load_step<C, true, kV>(p, pl, ids, t1, lane);
+    ids = find_blocks<C>(p, pl, min(j + 2 * stride, last));
+    body(t0, j);
     j += stride;
-    if (j >= j1) break;
-    a0 = next;
-    next = find_blocks<C>(pr, min(j + 2 * stride, last));
-    load_step<C, kV>(p, pr, a0, j + stride < j1, t0, lane);
-    body(t1, a1, j);
+    if (j + stride >= j1) return body(t1, j);
+    load_step<C, true, kV>(p, pl, ids, t0, lane);
+    ids = find_blocks<C>(p, pl, min(j + 2 * stride, last));
+    body(t1, j);
     j += stride;
-    if (j >= j1) break;
-    a1 = next;
+    if (j + stride >= j1) return body(t0, j);
   }
 }
 

@@ -4,6 +4,7 @@
 #pragma once
 
 #include "shaped.h"
+#include "shaped_slices.h"
 
 namespace neo {
 namespace {
@@ -27,12 +28,6 @@ __device__ inline PairIndex pair_index(const ShapedParams& p) {
 }
 
 template <class C>
-__device__ inline float natural_lse(const ShapedParams& p, int32_t g, int h, const Seen& seen,
-                                    float m, float l) {
-  return (m + __log2f(l)) * kLn2 + left_out<C>(p, g, h, seen);
-}
-
-template <class C>
 __global__ __launch_bounds__(kShapedThreads, 1) void attend_kernel(ShapedParams p) {
   constexpr int G = C::G;
   __shared__ float rows[kShapedWaves][G * kHeadDim];  // word c of row h at c ^ h
@@ -41,7 +36,7 @@ __global__ __launch_bounds__(kShapedThreads, 1) void attend_kernel(ShapedParams 
   const int lane = threadIdx.x & (kWave - 1);
   const int wv = uniform(threadIdx.x >> 6);
   const PairIndex at = pair_index(p);
-  const Seen seen = make_uniform(load_seen(p, at.b));
+  const Seen seen = load_seen(p, at.b);
   const int32_t row0 = at.b * p.hq + at.g * G;
   float* out = p.out + (size_t)row0 * kHeadDim;
   if (seen.n == 0) {
@@ -57,12 +52,13 @@ __global__ __launch_bounds__(kShapedThreads, 1) void attend_kernel(ShapedParams 
   const int32_t j1 = (int32_t)((int64_t)steps * (at.s + 1) / shares);
   const int waves = min(kShapedWaves, j1 - j0);  // with steps, the first ones
 
-  const Pair<C> pr = make_pair<C>(p, at.b, at.g, seen, lane);
+  const Place place{at.b, at.g, seen};
+  const Pair<C> pr = make_pair<C>(p, place, lane);
   Softmax st;
   st.init();
-  each_step<C, true>(p, pr, j0 + wv, j1, kShapedWaves, lane,
-                     [&](typename C::Tile& t, const Blocks<C>& blocks, int32_t j) {
-                       attend_step<C>(p, pr, t, blocks, j, st, lane);
+  each_step<C, true>(p, place, j0 + wv, j1, kShapedWaves, lane,
+                     [&](typename C::Tile& t, int32_t j) {
+                       attend_step<C>(p, seen, pr, t, j, st, lane);
                      });
   if (wv < waves) {
     C::fold(st.acc);
@@ -116,41 +112,8 @@ __global__ __launch_bounds__(kShapedThreads, 1) void attend_kernel(ShapedParams 
   __syncthreads();
   if (arrived != shares - 1) return;
   const size_t slot0 = (size_t)pair * p.parts;
-  for (int h = wv; h < G; h += kShapedWaves) {
-    float m = kLowest, l = 0.f, x = 0.f, y = 0.f;
-    for (int32_t base = 0; base < shares; base += kWave) {
-      const int32_t cnt = min(kWave, shares - base);
-      const size_t mine = slot0 + base + min(lane, cnt - 1);
-      const float2 ml = load_coherent2(p.part_ml + (mine * G + h) * 2);
-      const float mc = fmaxf(m, wave_max_f32(ml.x));
-      const float w = lane < cnt ? __builtin_amdgcn_exp2f(ml.x - mc) : 0.f;
-      const float scale = __builtin_amdgcn_exp2f(m - mc);  // 0 on the first round
-      m = mc;
-      l = l * scale + wave_sum_f32(lane < cnt ? w * ml.y : 0.f);
-      x *= scale;
-      y *= scale;
-      constexpr int kBatch = 16;
-      for (int32_t i0 = 0; i0 < cnt; i0 += kBatch) {
-        float2 v[kBatch];
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u)
-          v[u] = load_coherent2(p.part_o +
-                                ((slot0 + base + min(i0 + u, cnt - 1)) * G + h) * kHeadDim +
-                                2 * lane);
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-          if (i0 + u >= cnt) break;
-          const float wi = __builtin_bit_cast(
-              float, __builtin_amdgcn_readlane(__builtin_bit_cast(int32_t, w), i0 + u));
-          x = fmaf(wi, v[u].x, x);
-          y = fmaf(wi, v[u].y, y);
-        }
-      }
-    }
-    const float inv = 1.f / l;
-    *reinterpret_cast<float2*>(out + h * kHeadDim + 2 * lane) = float2{x * inv, y * inv};
-    if (p.lse && lane == 0) p.lse[row0 + h] = natural_lse<C>(p, at.g, h, seen, m, l);
-  }
+  for (int h = wv; h < G; h += kShapedWaves)
+    merge_row<C>(p, row0 + h, at.g, h, seen, shares, [&](int32_t i) { return slot0 + i; }, lane);
 }
 
 // Sum over the heads of a token's weights: lanes of the 16-lane row (or of each
@@ -178,14 +141,15 @@ __global__ __launch_bounds__(kShapedThreads, 1) void weights_kernel(ShapedParams
   const int lane = threadIdx.x & (kWave - 1);
   const int wv = uniform(threadIdx.x >> 6);
   const PairIndex at = pair_index(p);
-  const Seen seen = make_uniform(load_seen(p, at.b));
+  const Seen seen = load_seen(p, at.b);
   if (seen.n == 0) return;
   const int32_t steps = (seen.n - 1) / C::kStep + 1;
   const int32_t shares = shares_of(steps, p.parts);
   if (at.s >= shares) return;
   const int32_t j0 = (int32_t)((int64_t)steps * at.s / shares);
   const int32_t j1 = (int32_t)((int64_t)steps * (at.s + 1) / shares);
-  const Pair<C> pr = make_pair<C>(p, at.b, at.g, seen, lane);
+  const Place place{at.b, at.g, seen};
+  const Pair<C> pr = make_pair<C>(p, place, lane);
   const int h = C::head(lane), col = lane & 15;
   const bool real = h < C::G;
   // lse in base 2, without the bias of the pair's origin; one rounding, since
@@ -198,14 +162,17 @@ __global__ __launch_bounds__(kShapedThreads, 1) void weights_kernel(ShapedParams
   }
   const size_t row = ((size_t)at.b * p.hkv + at.g) * (size_t)p.sums_stride;
   each_step<C, false>(
-      p, pr, j0 + wv, j1, kShapedWaves, lane,
-      [&](typename C::Tile& t, const Blocks<C>& blocks, int32_t j) {
+      p, place, j0 + wv, j1, kShapedWaves, lane,
+      [&](typename C::Tile& t, int32_t j) {
         float x[C::kValues];
         const bool all = seen.sees_all(j * C::kStep, C::kStep);
-        shaped_scores<C>(p, pr, t, blocks, all, x, lane);
+        C::scores(t, pr.q, x, lane);
+        int32_t first[C::kStep];
+        first_tokens<C>(seen, j, first);
+        shape_scores<C>(p, seen, pr, first, all, x, lane);
 #pragma unroll
         for (int v = 0; v < C::kValues; v += 4) {
-          const int32_t t0 = C::position(v / 4, blocks.first, lane);
+          const int32_t t0 = C::position(v / 4, first, lane);
           float w[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i)
@@ -223,6 +190,10 @@ __global__ __launch_bounds__(kShapedThreads, 1) void weights_kernel(ShapedParams
 
 template <template <int> class Cache, int G>
 hipError_t launch_shaped_g(const ShapedParams& p, bool weights, hipStream_t stream) {
+  if (p.slices > 0 && !weights) {
+    slice_kernel<Cache<G>><<<p.slices, kWave * Cache<G>::kSliceWaves, 0, stream>>>(p);
+    return hipGetLastError();
+  }
   const unsigned grid = (unsigned)((int64_t)p.batch * p.hkv * p.parts);
   if (weights)
     weights_kernel<Cache<G>><<<grid, kShapedThreads, 0, stream>>>(p);
