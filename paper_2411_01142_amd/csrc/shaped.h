@@ -97,6 +97,13 @@ __device__ inline uint32_t from_xor8(uint32_t v) {
 __device__ inline float from_xor8(float v) {
   return __builtin_bit_cast(float, from_xor8(__builtin_bit_cast(uint32_t, v)));
 }
+// `other` of lane l ^ 8 in the upper (lower) eight lanes of each row, `own` in the rest.
+__device__ inline uint32_t upper_from_xor8(uint32_t own, uint32_t other) {
+  return (uint32_t)__builtin_amdgcn_update_dpp((int)own, (int)other, kDppRowRor8, 0xF, 0xC, false);
+}
+__device__ inline uint32_t lower_from_xor8(uint32_t own, uint32_t other) {
+  return (uint32_t)__builtin_amdgcn_update_dpp((int)own, (int)other, kDppRowRor8, 0xF, 0x3, false);
+}
 
 // tanh to fp32 accuracy in the absolute sense that scores need: odd Taylor
 // polynomial below 0.3 (the first term left out is 1e-8 of the value there),
@@ -257,6 +264,11 @@ struct PackedCache {
   __device__ static float scale_of(uint32_t exponent) {
     return __builtin_bit_cast(float, exponent << 23);
   }
+  // Of byte i of four. The conversions read a scale's exponent alone, so what the other
+  // bytes leave in its sign and mantissa does not matter.
+  __device__ static float scale_of_byte(uint32_t exponents, int i) {
+    return __builtin_bit_cast(float, i < 3 ? exponents << (23 - 8 * i) : exponents >> 1);
+  }
   // Eight 4-bit numbers times their scale.
   __device__ static bf16x8_t eight(uint32_t word, float scale) {
     const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 0);
@@ -321,10 +333,8 @@ struct PackedCache {
         split(w + 4 * pair, q);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const uint32_t keep = second ? q[1][i] : q[0][i];
-          const uint32_t got = from_xor8(second ? q[0][i] : q[1][i]);
-          part[0][i] = second ? got : keep;
-          part[0][2 + i] = second ? keep : got;
+          part[0][i] = upper_from_xor8(q[0][i], q[1][i]);
+          part[0][2 + i] = lower_from_xor8(q[1][i], q[0][i]);
           part[1][i] = second ? 0 : q[2][i];
           part[1][2 + i] = second ? q[2][i] : 0;
         }
@@ -345,7 +355,7 @@ struct PackedCache {
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          scale[b][i] = scale_of((x.ve[2 * pair + b] >> (8 * i)) & 0xFF);
+          scale[b][i] = scale_of_byte(x.ve[2 * pair + b], i);
       auto product = [&](int m, const u32x4_t& a) {
 #pragma unroll
         for (int k = 0; k < (kTwice ? 2 : 3); ++k)
@@ -501,14 +511,18 @@ __device__ inline void load_step(const ShapedParams& p, const Place& at, const B
 }
 
 // A step's products q.k become its scores, in base 2 and without the bias of the pair's
-// origin.
+// origin: x times the factor returned (that of plain scores is left to be multiplied
+// where the maximum is subtracted).
 template <class C>
-__device__ inline void shape_scores(const ShapedParams& p, const Seen& seen, const Pair<C>& pr,
+__device__ inline float shape_scores(const ShapedParams& p, const Seen& seen, const Pair<C>& pr,
                                     const int32_t (&first)[C::kStep], bool all,
                                     float (&x)[C::kValues], int lane) {
+  float factor = 1.f;
   if (p.cap_log2 != 0.f) {
 #pragma unroll
     for (int v = 0; v < C::kValues; ++v) x[v] = p.cap_log2 * tanh_score(x[v] * p.cap_in);
+  } else if (!p.slopes && p.scale_log2 > 0.f) {
+    factor = p.scale_log2;
   } else {
 #pragma unroll
     for (int v = 0; v < C::kValues; ++v) x[v] *= p.scale_log2;
@@ -530,6 +544,7 @@ __device__ inline void shape_scores(const ShapedParams& p, const Seen& seen, con
         if (!seen.sees(t0 + i)) x[v + i] = -INFINITY;
     }
   }
+  return factor;
 }
 
 // The running softmax of one head (and the sums of its lanes).
@@ -553,7 +568,7 @@ __device__ inline void attend_scores(const ShapedParams& p, const Seen& seen, co
   const bool all = seen.sees_all(j * C::kStep, C::kStep);
   int32_t first[C::kStep];
   first_tokens<C>(seen, j, first);
-  shape_scores<C>(p, seen, pr, first, all, x, lane);
+  const float factor = shape_scores<C>(p, seen, pr, first, all, x, lane);
   if (!all) {
 #pragma unroll
     for (int u = 0; u < C::kStep; ++u)
@@ -564,12 +579,12 @@ __device__ inline void attend_scores(const ShapedParams& p, const Seen& seen, co
   float mt = x[0];
 #pragma unroll
   for (int v = 1; v < C::kValues; ++v) mt = fmaxf(mt, x[v]);
-  const float mn = fmaxf(st.m, C::head_max(mt));
+  const float mn = fmaxf(st.m, C::head_max(mt) * factor);
   const float alpha = __builtin_amdgcn_exp2f(st.m - mn);
   float sum = 0.f;
 #pragma unroll
   for (int v = 0; v < C::kValues; ++v) {
-    x[v] = __builtin_amdgcn_exp2f(x[v] - mn);
+    x[v] = __builtin_amdgcn_exp2f(fmaf(x[v], factor, -mn));
     sum += x[v];
   }
   st.l = fmaf(st.l, alpha, sum);

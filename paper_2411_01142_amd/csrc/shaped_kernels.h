@@ -169,14 +169,14 @@ __global__ __launch_bounds__(kShapedThreads, 1) void weights_kernel(ShapedParams
         C::scores(t, pr.q, x, lane);
         int32_t first[C::kStep];
         first_tokens<C>(seen, j, first);
-        shape_scores<C>(p, seen, pr, first, all, x, lane);
+        const float factor = shape_scores<C>(p, seen, pr, first, all, x, lane);
 #pragma unroll
         for (int v = 0; v < C::kValues; v += 4) {
           const int32_t t0 = C::position(v / 4, first, lane);
           float w[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            w[i] = sum_over_columns<kHalves>(real ? __builtin_amdgcn_exp2f(x[v + i] - lse) : 0.f);
+            w[i] = sum_over_columns<kHalves>(real ? __builtin_amdgcn_exp2f(fmaf(x[v + i], factor, -lse)) : 0.f);
           // Columns 0-3 (and 8-11) write a token each.
           const int i = col & 3;
           const float mine = i < 2 ? (i == 0 ? w[0] : w[1]) : (i == 2 ? w[2] : w[3]);
