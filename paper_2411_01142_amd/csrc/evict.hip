@@ -17,6 +17,11 @@ namespace {
 constexpr int kSelectWaves = 16;
 constexpr int kSelectThreads = kWave * kSelectWaves;
 constexpr int kBins = 256;
+// Requests whose table allows up to this many tokens have their sums read once and kept in
+// LDS: 10.7 us for one request of 8 heads and 4099 tokens, where six passes over L2 take
+// 11.1, and 33 us against 37 for 96 requests of 2048 to 8192 tokens. (Counting 12 bits at
+// first and ranking the rest directly: 12.2 and 39; in registers, unrolled: 17.5 and 35.)
+constexpr int32_t kOnceTokens = 8192;
 
 // Unsigned integers in the order of the sums; both zeros are the same, and a NaN
 // counts as the largest, so that what is not understood stays.
@@ -31,7 +36,9 @@ __device__ inline int32_t kept_of(const EvictParams& p, int32_t b, int32_t L) {
   return min(L, min(max(p.budgets[b], 0), p.new_mbps * kBlock));
 }
 
+template <bool kOnce>
 __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictParams p) {
+  __shared__ float once[kOnce ? kOnceTokens : 1];
   __shared__ int32_t bins[kBins];
   __shared__ int32_t state[2];  // the bin that holds the k-th largest, what is left of k there
   __shared__ int32_t above[kSelectWaves], equal[kSelectWaves];
@@ -46,6 +53,12 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictParams p) {
   const float* sums = p.sums + ((size_t)b * p.hkv + g) * (size_t)p.sums_stride;
   int32_t* kept = p.kept + ((size_t)b * p.hkv + g) * (size_t)slots;
   float* new_sums = p.new_sums + ((size_t)b * p.hkv + g) * (size_t)slots;
+  auto sum_of = [&](int32_t t) { return kOnce ? once[t] : sums[t]; };
+  if constexpr (kOnce) {
+#pragma unroll 4
+    for (int32_t t = threadIdx.x; t < old; t += kSelectThreads) once[t] = sums[t];
+    __syncthreads();
+  }
   if (g == 0 && threadIdx.x == 0) p.new_lens[b] = n;
   for (int32_t i = n + threadIdx.x; i < slots; i += kSelectThreads) {
     kept[i] = -1;
@@ -60,7 +73,7 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictParams p) {
       for (int i = threadIdx.x; i < kBins; i += kSelectThreads) bins[i] = 0;
       __syncthreads();
       for (int32_t t = threadIdx.x; t < old; t += kSelectThreads) {
-        const uint32_t u = order_of(sums[t]);
+        const uint32_t u = order_of(sum_of(t));
         if (shift == 24 || (u >> (shift + 8)) == prefix)
           atomicAdd(&bins[(u >> shift) & 0xFF], 1);
       }
@@ -93,7 +106,7 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictParams p) {
   int32_t ca = 0, ce = 0;
   for (int32_t t0 = first; t0 < last; t0 += kWave) {
     const int32_t t = t0 + lane;
-    const uint32_t u = t < last ? order_of(sums[t]) : 0;
+    const uint32_t u = t < last ? order_of(sum_of(t)) : 0;
     ca += __popcll(__ballot(t < last && above_it(u)));
     ce += __popcll(__ballot(t < last && equal_it(u)));
   }
@@ -110,7 +123,7 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictParams p) {
   const uint64_t below = (1ull << lane) - 1;
   for (int32_t t0 = first; t0 < last; t0 += kWave) {
     const int32_t t = t0 + lane;
-    const float x = t < last ? sums[t] : 0.f;
+    const float x = t < last ? sum_of(t) : 0.f;
     const uint32_t u = order_of(x);
     const uint64_t eq = __ballot(t < last && equal_it(u));
     const bool stays = t < last && (above_it(u) || (equal_it(u) && seen_equal + __popcll(eq & below) < left));
@@ -219,7 +232,10 @@ __global__ __launch_bounds__(kWave* kMoveWaves) void move_kernel(EvictParams p) 
 }  // namespace
 
 hipError_t launch_evict(const EvictParams& p, bool packed, hipStream_t stream) {
-  select_kernel<<<(unsigned)(p.batch * p.hkv), kSelectThreads, 0, stream>>>(p);
+  if ((int64_t)p.mbps * kBlock <= kOnceTokens)
+    select_kernel<true><<<(unsigned)(p.batch * p.hkv), kSelectThreads, 0, stream>>>(p);
+  else
+    select_kernel<false><<<(unsigned)(p.batch * p.hkv), kSelectThreads, 0, stream>>>(p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int64_t tiles = (int64_t)p.batch * p.new_mbps * p.hkv;

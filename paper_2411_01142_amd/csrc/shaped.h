@@ -604,25 +604,25 @@ __device__ inline void attend_step(const ShapedParams& p, const Seen& seen, cons
   attend_scores<C>(p, seen, pr, t, j, x, st, lane);
 }
 
-// Steps j0, j0 + stride, ... below j1 of a pair, one step's tiles in flight ahead
-// of the one computed and the block ids another step ahead.
-template <class C, bool kV, class Body>
+// Steps j0, j0 + stride, ... below j1 of a pair: `load` requests a step's tile and `body`
+// uses it, one step in flight ahead of the one computed and block ids another ahead.
+template <class C, class Tile, class Load, class Body>
 __device__ inline void each_step(const ShapedParams& p, const Place& pl, int32_t j0, int32_t j1,
-                                 int32_t stride, int lane, Body body) {
+                                 int32_t stride, Load load, Body body) {
   if (j0 >= j1) return;
-  typename C::Tile t0, t1;
-  load_step<C, true, kV>(p, pl, find_blocks<C>(p, pl, j0), t0, lane);
+  Tile t0, t1;
+  load(t0, find_blocks<C>(p, pl, j0), j0);
   if (j0 + stride >= j1) return body(t0, j0);
   // (The last step stands outside of the loop, so that every step in it requests as much.)
   const int32_t last = j1 - 1;
   Blocks<C> ids = find_blocks<C>(p, pl, j0 + stride);
   for (int32_t j = j0;;) {
-    load_step<C, true, kV>(p, pl, ids, t1, lane);
+    load(t1, ids, j + stride);
     ids = find_blocks<C>(p, pl, min(j + 2 * stride, last));
     body(t0, j);
     j += stride;
     if (j + stride >= j1) return body(t1, j);
-    load_step<C, true, kV>(p, pl, ids, t0, lane);
+    load(t0, ids, j + stride);
     ids = find_blocks<C>(p, pl, min(j + 2 * stride, last));
     body(t1, j);
     j += stride;

@@ -56,10 +56,12 @@ __global__ __launch_bounds__(kShapedThreads, 1) void attend_kernel(ShapedParams 
   const Pair<C> pr = make_pair<C>(p, place, lane);
   Softmax st;
   st.init();
-  each_step<C, true>(p, place, j0 + wv, j1, kShapedWaves, lane,
-                     [&](typename C::Tile& t, int32_t j) {
-                       attend_step<C>(p, seen, pr, t, j, st, lane);
-                     });
+  each_step<C, typename C::Tile>(
+      p, place, j0 + wv, j1, kShapedWaves,
+      [&](typename C::Tile& t, const Blocks<C>& ids, int32_t) {
+        load_step<C, true, true>(p, place, ids, t, lane);
+      },
+      [&](typename C::Tile& t, int32_t j) { attend_step<C>(p, seen, pr, t, j, st, lane); });
   if (wv < waves) {
     C::fold(st.acc);
     const float l = C::head_sum(st.l);
@@ -161,27 +163,44 @@ __global__ __launch_bounds__(kShapedThreads, 1) void weights_kernel(ShapedParams
     lse = fmaf(-slope, d, p.lse_in[at.b * p.hq + at.g * C::G + h]) * 1.4426950408889634f;
   }
   const size_t row = ((size_t)at.b * p.hkv + at.g) * (size_t)p.sums_stride;
-  each_step<C, false>(
-      p, place, j0 + wv, j1, kShapedWaves, lane,
-      [&](typename C::Tile& t, int32_t j) {
-        float x[C::kValues];
-        const bool all = seen.sees_all(j * C::kStep, C::kStep);
-        C::scores(t, pr.q, x, lane);
+  // A step's sums are requested with its keys: read when they are needed, they would be
+  // waited for behind the next step's keys. Columns 0-3 (and 8-11) hold a token each.
+  constexpr int kGroups = C::kValues / 4;
+  struct Tile {
+    typename C::Tile k;
+    float sums[kGroups];
+  };
+  const int i = col & 3;
+  const bool writes = kHalves ? (col & 4) == 0 : col < 4;
+  const float* in = p.sums + row;
+  float* out = p.sums_out + row;
+  each_step<C, Tile>(
+      p, place, j0 + wv, j1, kShapedWaves,
+      [&](Tile& t, const Blocks<C>& ids, int32_t j) {
+        load_step<C, true, false>(p, place, ids, t.k, lane);
         int32_t first[C::kStep];
         first_tokens<C>(seen, j, first);
+#pragma unroll
+        for (int v = 0; v < kGroups; ++v)
+          t.sums[v] = in[min(C::position(v, first, lane) + i, seen.L - 1)];
+      },
+      [&](Tile& t, int32_t j) {
+        float x[C::kValues];
+        const bool all = seen.sees_all(j * C::kStep, C::kStep);
+        int32_t first[C::kStep];
+        first_tokens<C>(seen, j, first);
+        C::scores(t.k, pr.q, x, lane);
         const float factor = shape_scores<C>(p, seen, pr, first, all, x, lane);
 #pragma unroll
-        for (int v = 0; v < C::kValues; v += 4) {
-          const int32_t t0 = C::position(v / 4, first, lane);
+        for (int v = 0; v < kGroups; ++v) {
           float w[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            w[i] = sum_over_columns<kHalves>(real ? __builtin_amdgcn_exp2f(fmaf(x[v + i], factor, -lse)) : 0.f);
-          // Columns 0-3 (and 8-11) write a token each.
-          const int i = col & 3;
+          for (int u = 0; u < 4; ++u)
+            w[u] = sum_over_columns<kHalves>(
+                real ? __builtin_amdgcn_exp2f(fmaf(x[4 * v + u], factor, -lse)) : 0.f);
           const float mine = i < 2 ? (i == 0 ? w[0] : w[1]) : (i == 2 ? w[2] : w[3]);
-          const bool writes = kHalves ? (col & 4) == 0 : col < 4;
-          if (writes && seen.sees(t0 + i)) p.sums_out[row + t0 + i] = p.sums[row + t0 + i] + mine;
+          const int32_t at_t = C::position(v, first, lane) + i;
+          if (writes && seen.sees(at_t)) out[at_t] = t.sums[v] + mine;
         }
       });
 }

@@ -34,6 +34,7 @@ __all__ = [
 
 PACKED_RECORD_BYTES = 2176
 _BLOCK, _DIM = 16, 128
+_SCALE = 1.0 / math.sqrt(_DIM)
 
 
 class _ScoreShape(ctypes.Structure):
@@ -68,10 +69,24 @@ def declare(lib):
 
 # ------------------------------------------------------------------ checks
 
+# As in the package's own calls, a kernel can be shorter than the Python around it, so
+# the checks are written for the tensors that pass them: plain attributes compared once.
+# What does not pass goes through the full ones, which say what is wrong.
+
+_torch_module = None
+
+
+def _t():
+    global _torch_module
+    if _torch_module is None:
+        _torch_module = _neo._torch()
+    return _torch_module
+
+
 def _want(t, name, dtype, shape, device):
     """t's address if it is a contiguous tensor of this type and shape on ``device``."""
-    if (type(t) is _neo._torch().Tensor and t.dtype is dtype and t.device == device
-            and tuple(t.shape) == shape and t.is_contiguous()):
+    if (type(t) is _t().Tensor and t.dtype is dtype and t.shape == shape and t.device == device
+            and t.is_contiguous()):
         return t.data_ptr()
     _neo._require(t, name, dtype, len(shape))
     if tuple(t.shape) != shape:
@@ -81,37 +96,32 @@ def _want(t, name, dtype, shape, device):
     return t.data_ptr()
 
 
-def _maybe(t, name, dtype, shape, device):
-    return None if t is None else _want(t, name, dtype, shape, device)
-
-
 def _device_of(t, name):
-    torch = _neo._torch()
-    if not isinstance(t, torch.Tensor):
+    if not isinstance(t, _t().Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
-    if t.device.type != "cuda":
+    if not t.is_cuda:
         raise ValueError(f"{name} must be on a GPU (got {t.device}); there is no CPU path")
     return t.device
 
 
 def _bf16_caches(k_cache, v_cache):
     """(blocks, kv heads, block stride in elements); v_cache may be None."""
+    torch = _t()
+    shape, stride = k_cache.shape, k_cache.stride()
+    if (k_cache.dtype is torch.bfloat16 and len(shape) == 5 and shape[2:] == (16, 16, 8)
+            and stride[1:] == (2048, 128, 8, 1) and stride[0] % 8 == 0
+            and stride[0] >= shape[1] * 2048):
+        if v_cache is None:
+            return shape[0], shape[1], stride[0]
+        if (type(v_cache) is torch.Tensor and v_cache.dtype is torch.bfloat16
+                and v_cache.shape == (shape[0], shape[1], _DIM, _BLOCK)
+                and v_cache.stride() == (stride[0], 2048, 16, 1)
+                and v_cache.device == k_cache.device):
+            return shape[0], shape[1], stride[0]
     if v_cache is None:
-        stride = _neo._require_cache(k_cache, "k_cache", 5)
+        block_stride = _neo._require_cache(k_cache, "k_cache", 5)
     else:
-        torch = _neo._torch()
-        stride = None
-        if (type(k_cache) is torch.Tensor and type(v_cache) is torch.Tensor and k_cache.is_cuda
-                and k_cache.dtype is torch.bfloat16 and v_cache.dtype is torch.bfloat16
-                and k_cache.dim() == 5 and v_cache.dim() == 4):
-            h = k_cache.shape[1]
-            if (tuple(k_cache.shape[2:]) == (16, 16, 8) and v_cache.stride(0) == k_cache.stride(0)
-                    and k_cache.stride()[1:] == (2048, 128, 8, 1)
-                    and v_cache.stride()[1:] == (2048, 16, 1)
-                    and k_cache.stride(0) % 8 == 0 and k_cache.stride(0) >= h * 2048):
-                stride = k_cache.stride(0)
-        if stride is None:
-            stride = _neo._shared_stride(k_cache, "k_cache", v_cache, "v_cache")
+        block_stride = _neo._shared_stride(k_cache, "k_cache", v_cache, "v_cache")
     nb, hkv = k_cache.shape[:2]
     if tuple(k_cache.shape[2:]) != (_DIM // 8, _BLOCK, 8):
         raise ValueError(f"k_cache must be [blocks, kv heads, 16, 16, 8] (got {tuple(k_cache.shape)})")
@@ -120,42 +130,40 @@ def _bf16_caches(k_cache, v_cache):
             raise ValueError(f"v_cache shape {tuple(v_cache.shape)} != {(nb, hkv, _DIM, _BLOCK)}")
         if v_cache.device != k_cache.device:
             raise ValueError("k_cache and v_cache must be on one device")
-    return nb, hkv, stride
+    return nb, hkv, block_stride
 
 
 def _packed_cache(cache):
     """(blocks, kv heads, block stride in bytes)."""
-    torch = _neo._torch()
-    _device_of(cache, "cache")
-    if cache.dtype is not torch.uint8:
+    shape, stride = cache.shape, cache.stride()
+    if cache.dtype is not _t().uint8:
         raise TypeError(f"cache must be torch.uint8 (got {cache.dtype})")
-    if cache.dim() != 3 or cache.shape[2] != PACKED_RECORD_BYTES:
+    if len(shape) != 3 or shape[2] != PACKED_RECORD_BYTES:
         raise ValueError(f"cache must be [blocks, kv heads, {PACKED_RECORD_BYTES}] "
-                         f"(got {tuple(cache.shape)})")
-    nb, hkv, _ = cache.shape
-    stride = cache.stride(0)
-    if (cache.stride(2) != 1 or cache.stride(1) != PACKED_RECORD_BYTES
-            or stride < hkv * PACKED_RECORD_BYTES or stride % 16 != 0):
+                         f"(got {tuple(shape)})")
+    if (stride[1:] != (PACKED_RECORD_BYTES, 1) or stride[0] < shape[1] * PACKED_RECORD_BYTES
+            or stride[0] % 16 != 0):
         raise ValueError("cache must be dense within each block, with a block stride that is a "
-                         f"multiple of 16 bytes of at least one block (strides {cache.stride()})")
-    return nb, hkv, stride
+                         f"multiple of 16 bytes of at least one block (strides {stride})")
+    return shape[0], shape[1], stride[0]
 
 
 def _tables(block_table, seq_lens, device):
     """(batch, table width, addresses of both)."""
-    torch = _neo._torch()
+    torch = _t()
     if not isinstance(block_table, torch.Tensor):
         raise TypeError("block_table must be a torch.Tensor")
-    if block_table.dim() != 2:
-        raise ValueError(f"block_table must have 2 dims (got shape {tuple(block_table.shape)})")
-    B, width = block_table.shape
+    shape = block_table.shape
+    if len(shape) != 2:
+        raise ValueError(f"block_table must have 2 dims (got shape {tuple(shape)})")
+    B, width = shape
     return (B, width, _want(block_table, "block_table", torch.int32, (B, width), device),
             _want(seq_lens, "seq_lens", torch.int32, (B,), device))
 
 
-def _queries(q, hkv, B, device):
+def _queries(q, B, device):
     """(query heads, address)."""
-    torch = _neo._torch()
+    torch = _t()
     if not isinstance(q, torch.Tensor):
         raise TypeError("q must be a torch.Tensor")
     if q.dim() != 3:
@@ -165,16 +173,21 @@ def _queries(q, hkv, B, device):
 
 
 def _score_shape(softcap, slopes, starts, prefix_lens, B, hq, device):
-    torch = _neo._torch()
-    return _ScoreShape(0.0 if softcap is None else float(softcap),
-                       _maybe(slopes, "slopes", torch.float32, (hq,), device),
-                       _maybe(starts, "starts", torch.int32, (B,), device),
-                       _maybe(prefix_lens, "prefix_lens", torch.int32, (B,), device))
+    """The C structure, or None where scores are plain."""
+    if softcap is None and slopes is None and starts is None and prefix_lens is None:
+        return None
+    torch = _t()
+    return _ScoreShape(
+        0.0 if softcap is None else softcap,
+        None if slopes is None else _want(slopes, "slopes", torch.float32, (hq,), device),
+        None if starts is None else _want(starts, "starts", torch.int32, (B,), device),
+        None if prefix_lens is None else _want(prefix_lens, "prefix_lens", torch.int32, (B,),
+                                               device))
 
 
 def _new(shape, dtype, device, stream):
     """A tensor of the pool of the stream that is going to write it."""
-    torch = _neo._torch()
+    torch = _t()
     if stream is None:
         return torch.empty(shape, dtype=dtype, device=device)
     with torch.cuda.stream(stream):
@@ -182,7 +195,7 @@ def _new(shape, dtype, device, stream):
 
 
 def _capturing(stream):
-    torch = _neo._torch()
+    torch = _t()
     if stream is None:
         return torch.cuda.is_current_stream_capturing()
     with torch.cuda.stream(stream):
@@ -193,19 +206,19 @@ def _capturing(stream):
 
 def _attend(packed, q, caches, block_table, seq_lens, scale, out, softcap, slopes, starts,
             prefix_lens, lse, workspace, stream):
-    torch = _neo._torch()
+    torch = _t()
     lib = _neo._lib or _neo.load_library()
     device = _device_of(caches[0], "cache" if packed else "k_cache")
     nb, hkv, stride = _packed_cache(*caches) if packed else _bf16_caches(*caches)
     B, width, table_at, lens_at = _tables(block_table, seq_lens, device)
-    hq, q_at = _queries(q, hkv, B, device)
+    hq, q_at = _queries(q, B, device)
     shape = _score_shape(softcap, slopes, starts, prefix_lens, B, hq, device)
     if out is None:
         out = _new((B, hq, _DIM), torch.float32, device, stream)
         out_at = out.data_ptr()
     else:
         out_at = _want(out, "out", torch.float32, (B, hq, _DIM), device)
-    lse_at = _maybe(lse, "lse", torch.float32, (B, hq), device)
+    lse_at = None if lse is None else _want(lse, "lse", torch.float32, (B, hq), device)
     need = _neo._cached_workspace_bytes(B, hq, hkv, _DIM)
     if B == 0:
         return out
@@ -223,7 +236,7 @@ def _attend(packed, q, caches, block_table, seq_lens, scale, out, softcap, slope
             raise ValueError("all tensors must be on one device")
     fn = lib.neo_packed_decode_attention if packed else lib.neo_shaped_decode_attention
     args = (q_at, *(c.data_ptr() for c in caches), table_at, lens_at, hq, hkv, _DIM, _BLOCK,
-            1.0 / math.sqrt(_DIM) if scale is None else float(scale), shape, out_at, lse_at, B,
+            _SCALE if scale is None else scale, shape, out_at, lse_at, B,
             width, nb, stride, workspace.data_ptr(), workspace.numel(), handle)
     _neo._check(_neo._on_device(torch, device, fn, args))
     return out
@@ -258,7 +271,7 @@ def packed_decode_attention(q, cache, block_table, seq_lens, scale=None, out=Non
 def new_packed_kv_cache(num_blocks: int, num_kv_heads: int, device="cuda"):
     """A packed cache: uint8 ``[num_blocks, num_kv_heads, 2176]``, K and V of a block and kv
     head in one record (a quarter of the bf16 bytes and a sixteenth). Uninitialised."""
-    torch = _neo._torch()
+    torch = _t()
     return torch.empty((num_blocks, num_kv_heads, PACKED_RECORD_BYTES), dtype=torch.uint8,
                        device=device)
 
@@ -266,21 +279,22 @@ def new_packed_kv_cache(num_blocks: int, num_kv_heads: int, device="cuda"):
 def _row_strides(t, name, rows, hkv, device):
     """(row stride, head stride) in elements of bf16 rows [rows, Hkv, 128] that may be a view
     into something larger, such as a fused projection's output."""
-    torch = _neo._torch()
+    torch = _t()
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if t.device != device:
         raise ValueError(f"{name} must be on {device} (got {t.device})")
     if t.dtype is not torch.bfloat16:
         raise TypeError(f"{name} must be torch.bfloat16 (got {t.dtype})")
-    if t.dim() != 3 or (rows is not None and t.shape[0] != rows) or tuple(t.shape[1:]) != (hkv, _DIM):
+    shape = t.shape
+    if len(shape) != 3 or (rows is not None and shape[0] != rows) or shape[1:] != (hkv, _DIM):
         raise ValueError(f"{name} must be [{'rows' if rows is None else rows}, {hkv}, {_DIM}] "
-                         f"(got {tuple(t.shape)})")
+                         f"(got {tuple(shape)})")
     r, h, d = t.stride()
     if d != 1 or r % 8 != 0 or h % 8 != 0 or t.data_ptr() % 16 != 0:
         raise ValueError(f"{name} must have its dims in a run, strides that are multiples of 8 "
                          f"and 16-byte alignment (strides {t.stride()})")
-    return (r if t.shape[0] > 1 else 0), (h if hkv > 1 else 0)
+    return (r if shape[0] > 1 else 0), (h if hkv > 1 else 0)
 
 
 def packed_append(cache, k_new, v_new, block_table, seq_lens, row_starts=None, *, stream=None):
@@ -288,12 +302,14 @@ def packed_append(cache, k_new, v_new, block_table, seq_lens, row_starts=None, *
     cache, in place. Without ``row_starts`` row b is request b's newest token; with it (int32
     [B + 1], ascending), rows ``row_starts[b] .. row_starts[b + 1] - 1`` are its last tokens,
     as after a prompt. ``seq_lens`` counts them. Rows past ``row_starts[B]`` are skipped."""
-    torch = _neo._torch()
+    torch = _t()
     lib = _neo._lib or _neo.load_library()
     device = _device_of(cache, "cache")
     nb, hkv, stride = _packed_cache(cache)
     B, width, table_at, lens_at = _tables(block_table, seq_lens, device)
-    starts_at = _maybe(row_starts, "row_starts", torch.int32, (B + 1,), device)
+    starts_at = None
+    if row_starts is not None:
+        starts_at = _want(row_starts, "row_starts", torch.int32, (B + 1,), device)
     kr, kh = _row_strides(k_new, "k_new", None if row_starts is not None else B, hkv, device)
     rows = k_new.shape[0]
     vr, vh = _row_strides(v_new, "v_new", rows, hkv, device)
@@ -309,12 +325,14 @@ def packed_gather(cache, block_table, seq_lens, row_starts=None, k_out=None, v_o
     ``row_starts`` and lengths would write, read back exactly. The number of rows is that of
     ``k_out`` and ``v_out``, or ``rows``, or without ``row_starts`` the batch. Rows that have no
     token are left as they were (new outputs: zero)."""
-    torch = _neo._torch()
+    torch = _t()
     lib = _neo._lib or _neo.load_library()
     device = _device_of(cache, "cache")
     nb, hkv, stride = _packed_cache(cache)
     B, width, table_at, lens_at = _tables(block_table, seq_lens, device)
-    starts_at = _maybe(row_starts, "row_starts", torch.int32, (B + 1,), device)
+    starts_at = None
+    if row_starts is not None:
+        starts_at = _want(row_starts, "row_starts", torch.int32, (B + 1,), device)
     for t in (k_out, v_out):
         if t is not None and rows is None:
             rows = t.shape[0]
@@ -343,7 +361,7 @@ def packed_gather(cache, block_table, seq_lens, row_starts=None, k_out=None, v_o
 # ---------------------------------------------------------------- eviction
 
 def _sums_stride(sums, name, B, hkv, width, device):
-    torch = _neo._torch()
+    torch = _t()
     if not isinstance(sums, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if sums.dim() != 3 or sums.shape[2] < width * _BLOCK:
@@ -355,12 +373,12 @@ def _sums_stride(sums, name, B, hkv, width, device):
 
 def _add_weights(packed, sums, lse, q, cache, block_table, seq_lens, scale, out, softcap, slopes,
                  starts, prefix_lens, stream):
-    torch = _neo._torch()
+    torch = _t()
     lib = _neo._lib or _neo.load_library()
     device = _device_of(cache, "cache" if packed else "k_cache")
     nb, hkv, stride = _packed_cache(cache) if packed else _bf16_caches(cache, None)
     B, width, table_at, lens_at = _tables(block_table, seq_lens, device)
-    hq, q_at = _queries(q, hkv, B, device)
+    hq, q_at = _queries(q, B, device)
     S = _sums_stride(sums, "sums", B, hkv, width, device)
     if out is None:
         out = sums
@@ -373,7 +391,7 @@ def _add_weights(packed, sums, lse, q, cache, block_table, seq_lens, scale, out,
     shape = _score_shape(softcap, slopes, starts, prefix_lens, B, hq, device)
     fn = lib.neo_packed_add_attention_weights if packed else lib.neo_add_attention_weights
     args = (sums.data_ptr(), out.data_ptr(), S, lse_at, q_at, cache.data_ptr(), table_at, lens_at,
-            hq, hkv, _DIM, _BLOCK, 1.0 / math.sqrt(_DIM) if scale is None else float(scale), shape,
+            hq, hkv, _DIM, _BLOCK, _SCALE if scale is None else scale, shape,
             B, width, nb, stride, _neo._raw_stream(torch, stream, device))
     _neo._check(_neo._on_device(torch, device, fn, args))
     return out
@@ -399,7 +417,7 @@ def packed_add_attention_weights(sums, lse, q, cache, block_table, seq_lens, sca
 
 
 def _evict(packed, caches, block_table, seq_lens, sums, budgets, new_table, recent, stream):
-    torch = _neo._torch()
+    torch = _t()
     lib = _neo._lib or _neo.load_library()
     device = _device_of(caches[0], "cache" if packed else "k_cache")
     nb, hkv, stride = _packed_cache(*caches) if packed else _bf16_caches(*caches)
