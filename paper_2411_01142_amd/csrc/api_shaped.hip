@@ -172,7 +172,6 @@ neo_status attend(const void* q, const Cache& cache, bool packed, const int32_t*
   // compute unit, where the workspace has NEO_MAX_SLICES counters and as many
   // slots of rows, maxima and denominators.)
   p.parts = parts_of(batch, hkv, mbps, packed ? 4 : 1, std::min(cus, NEO_MAX_SLICES));
-  p.xcd8 = xcds == 8;
   p.slices = (int64_t)batch * hkv > cus ? std::min(cus, kMostSliceGroups) : 0;
   hipStream_t s = static_cast<hipStream_t>(stream);
   return launched(packed ? launch_shaped_packed(p, group, false, s)

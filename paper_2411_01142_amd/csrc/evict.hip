@@ -32,10 +32,6 @@ __device__ inline uint32_t order_of(float x) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-__device__ inline int32_t kept_of(const EvictParams& p, int32_t b, int32_t L) {
-  return min(L, min(max(p.budgets[b], 0), p.new_mbps * kBlock));
-}
-
 template <bool kOnce>
 __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictParams p) {
   __shared__ float once[kOnce ? kOnceTokens : 1];
@@ -46,7 +42,7 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictParams p) {
   const int wv = uniform(threadIdx.x >> 6);
   const int32_t b = blockIdx.x / p.hkv, g = blockIdx.x % p.hkv;
   const int32_t L = uniform(clamp_len(p.lens[b], p.mbps));
-  const int32_t n = uniform(kept_of(p, b, L));
+  const int32_t n = uniform(min(L, min(max(p.budgets[b], 0), p.new_mbps * kBlock)));
   const int32_t old = L - min(max(p.recent, 0), n);  // tokens that compete
   const int32_t k = n - (L - old);                   // and how many of them stay
   const int32_t slots = p.new_mbps * kBlock;
@@ -155,20 +151,17 @@ __global__ __launch_bounds__(kWave* kMoveWaves) void move_kernel(EvictParams p) 
   const int64_t b64 = rest / p.new_mbps;
   if (b64 >= p.batch) return;
   const int32_t b = (int32_t)b64;
-  const int32_t L = clamp_len(p.lens[b], p.mbps);
-  const int32_t n = kept_of(p, b, L);
-  if (j * kBlock >= n) return;
-  const int32_t dst_blk = p.new_table[(size_t)b * p.new_mbps + j];
-  if (dst_blk < 0 || dst_blk >= p.num_blocks) return;
-  // Lane l holds the place of token l % 16 of the new block.
-  const int32_t mine = j * kBlock + (lane & 15);
+  // Lane l holds the place of token l % 16 of the new block, -1 behind the new length.
   const int32_t src =
-      mine < n ? p.kept[((size_t)b * p.hkv + g) * (size_t)(p.new_mbps * kBlock) + mine] : 0;
-  const bool real = mine < n;
-  const int32_t sblk = p.table[(size_t)b * p.mbps + src / kBlock];
+      p.kept[((size_t)b * p.hkv + g) * (size_t)(p.new_mbps * kBlock) + j * kBlock + (lane & 15)];
+  const int32_t dst_blk = p.new_table[(size_t)b * p.new_mbps + j];
+  const bool real = src >= 0;
+  const int count = __popcll(__ballot(real)) / 4;  // tokens of the block, the first ones
+  if (count == 0 || dst_blk < 0 || dst_blk >= p.num_blocks) return;
+  const int32_t sblk = p.table[(size_t)b * p.mbps + max(src, 0) / kBlock];
   const int64_t from = (int64_t)min((uint32_t)sblk, (uint32_t)(p.num_blocks - 1)) * p.blk_bytes +
                        (int64_t)g * (kPacked ? kPackedRecord : kTileBytes);
-  const int sslot = src % kBlock;
+  const int sslot = src & (kBlock - 1);
   uint8_t* to = p.k + (int64_t)dst_blk * p.blk_bytes + (int64_t)g * (kPacked ? kPackedRecord : kTileBytes);
   auto from_of = [&](int slot) -> int64_t {
     const int32_t lo = __shfl((int32_t)(uint32_t)from, slot), hi = __shfl((int32_t)(from >> 32), slot);
@@ -190,7 +183,7 @@ __global__ __launch_bounds__(kWave* kMoveWaves) void move_kernel(EvictParams p) 
       const int slot = 4 * grp + i;
       const uint8_t* vrec = p.k + from_of(slot);
       const int ss = __shfl(sslot, slot);
-      if (j * kBlock + slot < n) {
+      if (slot < count) {
         v[i] = *reinterpret_cast<const uint32_t*>(vrec + packed_v_at(ss, r));
         if (r < 4) ve |= (uint32_t)vrec[packed_v_exp_at(ss, r)] << (8 * i);
       }
@@ -217,9 +210,8 @@ __global__ __launch_bounds__(kWave* kMoveWaves) void move_kernel(EvictParams p) 
       for (int slot = 0; slot < kBlock; ++slot) {
         const uint8_t* vrec = p.v + from_of(slot);
         const int ss = __shfl(sslot, slot);
-        uint32_t x = 0;
-        if (j * kBlock + slot < n)
-          x = *reinterpret_cast<const uint16_t*>(vrec + (d * kBlock + ss) * 2);
+        uint32_t x = *reinterpret_cast<const uint16_t*>(vrec + (d * kBlock + ss) * 2);
+        if (slot >= count) x = 0;
         w[slot / 2] = slot % 2 ? w[slot / 2] | (x << 16) : x;
       }
       u32x4_t* dst = reinterpret_cast<u32x4_t*>(vto + d * kBlock * 2);

@@ -34,7 +34,6 @@ struct ShapedParams {
   int64_t sums_stride;
   int32_t batch, hq, hkv, mbps, num_blocks;
   int32_t parts;            // workgroups of a (request, kv head) pair, at most
-  int32_t xcd8;             // the device has eight XCDs
   int32_t slices;           // workgroups of a call in slices, 0: in pairs
   float scale_log2;         // scale * log2(e)
   float cap_in, cap_log2;   // scale / cap and cap * log2(e); cap_log2 0: no cap
@@ -120,6 +119,24 @@ __device__ inline float tanh_score(float y) {
   return fabsf(y) < 0.3f ? small : big;
 }
 
+// Four weights as sums of three bf16 numbers each, the leading eight of their 24 bits, the
+// next and the last, so that nothing of them is lost; two to a register. (With two parts,
+// 16 bits, a result is off by 1 to 2.5e-6 of itself, with three by the fp32 sums'
+// roundings.)
+__device__ inline void split_weights(const float* w, uint32_t (&parts)[3][2]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    float a = w[2 * i], b = w[2 * i + 1];
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      const uint32_t ua = __builtin_bit_cast(uint32_t, a), ub = __builtin_bit_cast(uint32_t, b);
+      parts[k][i] = __builtin_amdgcn_perm(ub, ua, 0x07060302);
+      a -= __builtin_bit_cast(float, ua & 0xFFFF0000u);
+      b -= __builtin_bit_cast(float, ub & 0xFFFF0000u);
+    }
+  }
+}
+
 // ------------------------------------------------------------------ caches
 
 // A cache type provides the matrix products over a step of kStep blocks. Each
@@ -183,20 +200,15 @@ struct Bf16Cache {
   }
   __device__ static float head_max(float v) { return max_over_rows(v); }
   __device__ static float head_sum(float v) { return sum_over_rows(v); }
-  // Weights enter the product as three bf16 numbers each, of 8 bits more and more: with
-  // two, a result is off by 1 to 2.5e-6 of itself, with three by the fp32 sums' roundings.
   __device__ static void add_values(f32x4_t (&acc)[8], const Tile& x, const float (&w)[kValues],
                                     int) {
+    uint32_t q[3][2];
+    split_weights(w, q);
     s16x4_t part[3];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float rest = w[i];
-#pragma unroll
-      for (int k = 0; k < 3; ++k) {
-        const __bf16 h = (__bf16)rest;
-        part[k][i] = __builtin_bit_cast(short, h);
-        rest -= (float)h;
-      }
+    for (int k = 0; k < 3; ++k) {
+      const uint64_t two = (uint64_t)q[k][1] << 32 | q[k][0];
+      part[k] = __builtin_bit_cast(s16x4_t, two);
     }
 #pragma unroll
     for (int mb = 0; mb < 8; ++mb)
@@ -330,7 +342,7 @@ struct PackedCache {
       u32x4_t part[3];
       if constexpr (kTwice) {
         uint32_t q[3][2];
-        split(w + 4 * pair, q);
+        split_weights(w + 4 * pair, q);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           part[0][i] = upper_from_xor8(q[0][i], q[1][i]);
@@ -342,7 +354,7 @@ struct PackedCache {
         uint32_t q[3][2];
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-          split(w + 8 * pair + 4 * b, q);
+          split_weights(w + 8 * pair + 4 * b, q);
 #pragma unroll
           for (int k = 0; k < 3; ++k) {
             part[k][2 * b] = q[k][0];
@@ -389,20 +401,6 @@ struct PackedCache {
   __device__ static uint32_t pair_of(uint32_t word, float scale) {
     return __builtin_bit_cast(uint32_t,
                               __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, kByte));
-  }
-  // Four weights as sums of three bf16 numbers, two to a register.
-  __device__ static void split(const float* w, uint32_t (&parts)[3][2]) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      float a = w[2 * i], b = w[2 * i + 1];
-#pragma unroll
-      for (int k = 0; k < 3; ++k) {
-        const bf16x2_t h = {(__bf16)a, (__bf16)b};
-        parts[k][i] = __builtin_bit_cast(uint32_t, h);
-        a -= (float)h[0];
-        b -= (float)h[1];
-      }
-    }
   }
   __device__ static void fold(f32x4_t (&acc)[8]) {
     if constexpr (kTwice) {
@@ -501,6 +499,9 @@ __device__ inline void first_tokens(const Seen& seen, int32_t j, int32_t (&first
 template <class C, bool kK, bool kV>
 __device__ inline void load_step(const ShapedParams& p, const Place& at, const Blocks<C>& blocks,
                                  typename C::Tile& t, int lane) {
+  // (Keeps the lanes' offsets from being widened to 64 bits ahead of a loop, which costs an
+  // addition a load in it: a load adds 32 bits to a uniform base itself.)
+  asm volatile("" : "+v"(lane));
 #pragma unroll
   for (int u = 0; u < C::kStep; ++u) {
     const uint32_t id = min((uint32_t)blocks.id[u], (uint32_t)(p.num_blocks - 1));
@@ -600,7 +601,11 @@ template <class C>
 __device__ inline void attend_step(const ShapedParams& p, const Seen& seen, const Pair<C>& pr,
                                    typename C::Tile& t, int32_t j, Softmax& st, int lane) {
   float x[C::kValues];
+  // Ahead of the other wavefronts of a SIMD, which so come to stand at other places of
+  // their steps (packed, 512 x U[256, 4096]: 227 -> 223 us; a window of 1500: 212 -> 210).
+  __builtin_amdgcn_s_setprio(1);
   C::scores(t, pr.q, x, lane);
+  __builtin_amdgcn_s_setprio(0);
   attend_scores<C>(p, seen, pr, t, j, x, st, lane);
 }
 
