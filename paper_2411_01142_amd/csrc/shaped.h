@@ -33,7 +33,8 @@ struct ShapedParams {
   const float* lse_in;      // [batch][hq]
   int64_t sums_stride;
   int32_t batch, hq, hkv, mbps, num_blocks;
-  int32_t parts;            // workgroups of a (request, kv head) pair, at most
+  int32_t parts;            // workgroups of a (request, kv head) pair of usual length
+  int32_t spare;            // and of all the longer ones together, more than that
   int32_t slices;           // workgroups of a call in slices, 0: in pairs
   float scale_log2;         // scale * log2(e)
   float cap_in, cap_log2;   // scale / cap and cap * log2(e); cap_log2 0: no cap

@@ -1,6 +1,6 @@
-// Kernels of attention with shaped scores, and of the sums of its weights, over
-// either cache type: a workgroup of eight wavefronts takes a (request, kv head)
-// pair or one of `parts` equal shares of it.
+// Kernels of attention with shaped scores, and of the sums of its weights, over either
+// cache type. Attention of few pairs: a workgroup of eight wavefronts takes a (request,
+// kv head) pair or one of several equal shares of it.
 #pragma once
 
 #include "shaped.h"
@@ -14,17 +14,49 @@ constexpr int kShapedThreads = kWave * kShapedWaves;
 // A share has at least this many steps for every wavefront.
 constexpr int32_t kStepsPerWave = 2;
 
-// Workgroups that share `steps` steps of a pair.
-__device__ inline int32_t shares_of(int32_t steps, int32_t parts) {
-  return min(parts, (steps - 1) / (kShapedWaves * kStepsPerWave) + 1);
-}
-
-struct PairIndex {
-  int32_t s, g, b;
+// A workgroup's share of a pair, the s-th of n, and what the request sees.
+struct Share {
+  int32_t b, g, s, n;
+  Seen seen;
 };
-__device__ inline PairIndex pair_index(const ShapedParams& p) {
-  const int32_t pair = blockIdx.x / p.parts;
-  return {(int32_t)blockIdx.x - pair * p.parts, pair % p.hkv, pair / p.hkv};
+// A pair has as many shares as `parts` and its steps allow; where it is so much longer than
+// the others that a share would be more than two compute units' part of the whole call, it
+// has more, and `spare` workgroups are there for those. (32 requests of 8 pairs, all of 512
+// tokens but one of 100000: 92 us, 891 with `parts` alone; packed 38 and 380.) All wavefronts find the same; false where nothing
+// is left for the workgroup.
+template <class C>
+__device__ inline bool find_share(const ShapedParams& p, int lane, Share& r) {
+  auto seen_by = [&](int32_t b) {
+    return b < p.batch ? lane_seen(p, b) : Seen{0, 0, 0, 0, 0, 0};
+  };
+  const Seen first = seen_by(lane);
+  int32_t total = steps_of<C>(first.n);
+  for (int32_t b = kWave + lane; b < p.batch; b += kWave) total += steps_of<C>(seen_by(b).n);
+  total = uniform(wave_sum_i32(total)) * p.hkv;
+  const int32_t limit = max(kShapedWaves * kStepsPerWave, total / p.spare + 1);
+  const int32_t wg = (int32_t)blockIdx.x;
+  int32_t before = 0;  // workgroups of the requests before
+  for (int32_t b0 = 0; b0 < p.batch; b0 += kWave) {
+    const Seen seen = b0 == 0 ? first : seen_by(b0 + lane);
+    const int32_t steps = steps_of<C>(seen.n);
+    const int32_t most = min(p.parts, (steps - 1) / (kShapedWaves * kStepsPerWave) + 1);
+    const int32_t n = b0 + lane < p.batch ? max(1, max(most, (steps - 1) / limit + 1)) : 0;
+    const int32_t incl = wave_incl_scan_i32(n);
+    const uint64_t behind = __ballot((before + incl) * p.hkv > wg);
+    if (behind) {
+      const int f = __builtin_ctzll(behind);
+      auto of = [&](int32_t v) { return __builtin_amdgcn_readlane(v, f); };
+      r.n = of(n);
+      const int32_t rem = wg - (before + of(incl) - r.n) * p.hkv;
+      r.b = b0 + f;
+      r.g = rem / r.n;
+      r.s = rem % r.n;
+      r.seen = Seen{of(seen.L), of(seen.p), of(seen.s), of(seen.pb), of(seen.f), of(seen.n)};
+      return true;
+    }
+    before += __builtin_amdgcn_readlane(incl, kWave - 1);
+  }
+  return false;
 }
 
 template <class C>
@@ -35,19 +67,17 @@ __global__ __launch_bounds__(kShapedThreads, 1) void attend_kernel(ShapedParams 
   __shared__ int32_t arrived;
   const int lane = threadIdx.x & (kWave - 1);
   const int wv = uniform(threadIdx.x >> 6);
-  const PairIndex at = pair_index(p);
-  const Seen seen = load_seen(p, at.b);
+  Share at;
+  if (!find_share<C>(p, lane, at)) return;
+  const Seen& seen = at.seen;
   const int32_t row0 = at.b * p.hq + at.g * G;
   float* out = p.out + (size_t)row0 * kHeadDim;
   if (seen.n == 0) {
-    if (at.s != 0) return;
     for (int i = threadIdx.x; i < G * kHeadDim; i += kShapedThreads) out[i] = 0.f;
     if (p.lse && threadIdx.x < G) p.lse[row0 + threadIdx.x] = -INFINITY;
     return;
   }
-  const int32_t steps = (seen.n - 1) / C::kStep + 1;
-  const int32_t shares = shares_of(steps, p.parts);
-  if (at.s >= shares) return;
+  const int32_t steps = steps_of<C>(seen.n), shares = at.n;
   const int32_t j0 = (int32_t)((int64_t)steps * at.s / shares);
   const int32_t j1 = (int32_t)((int64_t)steps * (at.s + 1) / shares);
   const int waves = min(kShapedWaves, j1 - j0);  // with steps, the first ones
@@ -78,7 +108,7 @@ __global__ __launch_bounds__(kShapedThreads, 1) void attend_kernel(ShapedParams 
   }
   __syncthreads();
   const int32_t pair = at.b * p.hkv + at.g;
-  const size_t slot = (size_t)pair * p.parts + at.s;
+  const size_t slot = blockIdx.x;
   for (int h = wv; h < G; h += kShapedWaves) {
     float m = kLowest, l = 0.f, x = 0.f, y = 0.f;
     for (int w = 0; w < waves; ++w) m = fmaxf(m, ms[w][h]);
@@ -113,7 +143,7 @@ __global__ __launch_bounds__(kShapedThreads, 1) void attend_kernel(ShapedParams 
   }
   __syncthreads();
   if (arrived != shares - 1) return;
-  const size_t slot0 = (size_t)pair * p.parts;
+  const size_t slot0 = slot - at.s;
   for (int h = wv; h < G; h += kShapedWaves)
     merge_row<C>(p, row0 + h, at.g, h, seen, shares, [&](int32_t i) { return slot0 + i; }, lane);
 }
@@ -135,23 +165,12 @@ __device__ inline float sum_over_columns(float v) {
   return v;
 }
 
-// sums_out[b][g][t] = sums[b][g][t] + sum over the group's heads of exp(x_t - lse),
-// for the tokens that the request sees. Reads K alone.
+// The weights of steps [j0, j1) of a pair, added to their sums.
 template <class C>
-__global__ __launch_bounds__(kShapedThreads, 1) void weights_kernel(ShapedParams p) {
-  constexpr bool kHalves = C::kValues == 8;
-  const int lane = threadIdx.x & (kWave - 1);
-  const int wv = uniform(threadIdx.x >> 6);
-  const PairIndex at = pair_index(p);
-  const Seen seen = load_seen(p, at.b);
-  if (seen.n == 0) return;
-  const int32_t steps = (seen.n - 1) / C::kStep + 1;
-  const int32_t shares = shares_of(steps, p.parts);
-  if (at.s >= shares) return;
-  const int32_t j0 = (int32_t)((int64_t)steps * at.s / shares);
-  const int32_t j1 = (int32_t)((int64_t)steps * (at.s + 1) / shares);
-  const Place place{at.b, at.g, seen};
-  const Pair<C> pr = make_pair<C>(p, place, lane);
+__device__ inline void add_weights(const ShapedParams& p, const Place& at, int32_t j0, int32_t j1,
+                                   int lane) {
+  const Seen& seen = at.seen;
+  const Pair<C> pr = make_pair<C>(p, at, lane);
   const int h = C::head(lane), col = lane & 15;
   const bool real = h < C::G;
   // lse in base 2, without the bias of the pair's origin; one rounding, since
@@ -165,6 +184,7 @@ __global__ __launch_bounds__(kShapedThreads, 1) void weights_kernel(ShapedParams
   const size_t row = ((size_t)at.b * p.hkv + at.g) * (size_t)p.sums_stride;
   // A step's sums are requested with its keys: read when they are needed, they would be
   // waited for behind the next step's keys. Columns 0-3 (and 8-11) hold a token each.
+  constexpr bool kHalves = C::kValues == 8;
   constexpr int kGroups = C::kValues / 4;
   struct Tile {
     typename C::Tile k;
@@ -175,9 +195,9 @@ __global__ __launch_bounds__(kShapedThreads, 1) void weights_kernel(ShapedParams
   const float* in = p.sums + row;
   float* out = p.sums_out + row;
   each_step<C, Tile>(
-      p, place, j0 + wv, j1, kShapedWaves,
+      p, at, j0, j1, 1,
       [&](Tile& t, const Blocks<C>& ids, int32_t j) {
-        load_step<C, true, false>(p, place, ids, t.k, lane);
+        load_step<C, true, false>(p, at, ids, t.k, lane);
         int32_t first[C::kStep];
         first_tokens<C>(seen, j, first);
 #pragma unroll
@@ -205,6 +225,31 @@ __global__ __launch_bounds__(kShapedThreads, 1) void weights_kernel(ShapedParams
       });
 }
 
+// sums_out[b][g][t] = sums[b][g][t] + sum over the group's heads of exp(x_t - lse),
+// for the tokens that the request sees. Reads K alone. Equal slices of the batch's steps,
+// one per wavefront, as of attention over large batches; tokens need no merging.
+template <class C>
+__global__ __launch_bounds__(kWave* C::kSliceWaves) void weights_kernel(ShapedParams p) {
+  const int lane = threadIdx.x & (kWave - 1);
+  LineStart at;
+  if (!find_slice<C>(p, at)) return;
+  Place pl{at.b, at.g, load_seen(p, at.b)};
+  for (int32_t first = at.s0 - at.x + kSlicePairCost;;) {
+    const int32_t steps = steps_of<C>(pl.seen.n);
+    add_weights<C>(p, pl, max(0, at.s0 - first), min(steps, at.s1 - first), lane);
+    first += steps;  // the next pair's position
+    if (first >= at.s1) return;
+    first += kSlicePairCost;
+    if (++pl.g == p.hkv) {
+      pl.g = 0;
+      do {
+        if (++pl.b >= p.batch) return;
+        pl.seen = load_seen(p, pl.b);
+      } while (pl.seen.n == 0);
+    }
+  }
+}
+
 }  // namespace
 
 template <template <int> class Cache, int G>
@@ -213,11 +258,11 @@ hipError_t launch_shaped_g(const ShapedParams& p, bool weights, hipStream_t stre
     slice_kernel<Cache<G>><<<p.slices, kWave * Cache<G>::kSliceWaves, 0, stream>>>(p);
     return hipGetLastError();
   }
-  const unsigned grid = (unsigned)((int64_t)p.batch * p.hkv * p.parts);
   if (weights)
-    weights_kernel<Cache<G>><<<grid, kShapedThreads, 0, stream>>>(p);
+    weights_kernel<Cache<G>><<<p.slices, kWave * Cache<G>::kSliceWaves, 0, stream>>>(p);
   else
-    attend_kernel<Cache<G>><<<grid, kShapedThreads, 0, stream>>>(p);
+    attend_kernel<Cache<G>>
+        <<<p.batch * p.hkv * p.parts + p.spare, kShapedThreads, 0, stream>>>(p);
   return hipGetLastError();
 }
 
