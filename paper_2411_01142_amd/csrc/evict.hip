@@ -7,6 +7,13 @@
 // order; equal sums stay from the lowest token on. The second moves the tokens'
 // keys and values, one wavefront per new (block, kv head) tile. Source blocks are
 // only read, so blocks that several requests share may be evicted from.
+//
+// One row's selection is a chain of four rounds, each a pass and two barriers; a workgroup
+// per row leaves most of the chip idle for small batches, and other splits would pay the
+// same barriers across workgroups. The move is bound by HBM's lines: a packed token is 136
+// bytes in 34 pieces of a record, and of 16 tokens scattered over their blocks nearly every
+// line is fetched whole (96 requests of 2048 to 8192 tokens to 1500: 124 us for 339 MB of
+// tokens, about 690 MB of lines, 5.6 TB/s).
 #include "decode_common.h"
 #include "packed.h"
 #include "shaped_ops.h"

@@ -8,7 +8,9 @@ namespace {
 
 // A workgroup takes 16 rows of one kv head, which in a prompt are a block or parts
 // of two, so that the bytes of a record's lines meet in one L2; 16 threads a row,
-// 8 dims each.
+// 8 dims each. Prompts are bound by HBM (five of 1000 to 6000 tokens, 8 kv heads: written
+// 18.6 us, read back 15.5, 4.3 and 5.2 TB/s); a token for each of 256 requests by latency
+// (3.2 and 2.8 us).
 constexpr int kRowsPerGroup = 16;
 constexpr int kRowThreads = kHeadDim / 8;
 

@@ -1,6 +1,9 @@
 // Kernels of attention with shaped scores, and of the sums of its weights, over either
 // cache type. Attention of few pairs: a workgroup of eight wavefronts takes a (request,
-// kv head) pair or one of several equal shares of it.
+// kv head) pair or one of several equal shares of it. Such calls are short, and most of
+// their time is latency: lengths, block ids, the first tiles, the merge in LDS and, between
+// workgroups, through the workspace (one request of 877 tokens, 32/8 heads 8.9 us; packed, of
+// 50021 tokens 18 us, where the loads alone take 16).
 #pragma once
 
 #include "shaped.h"
@@ -227,7 +230,11 @@ __device__ inline void add_weights(const ShapedParams& p, const Place& at, int32
 
 // sums_out[b][g][t] = sums[b][g][t] + sum over the group's heads of exp(x_t - lse),
 // for the tokens that the request sees. Reads K alone. Equal slices of the batch's steps,
-// one per wavefront, as of attention over large batches; tokens need no merging.
+// one per wavefront, as of attention over large batches; tokens need no merging. 64 requests
+// of U[512, 2048] tokens, 32/8 heads: 32.5 us, 5.8 TB/s of keys and sums. Packed, 256 of
+// U[256, 4096], 64/8 heads, capped: 69 us, 4.9 TB/s, or 5.1 with the whole lines of which the
+// keys' exponents take half; the tanh of each score costs as much as its products. (A
+// workgroup per pair: 77.)
 template <class C>
 __global__ __launch_bounds__(kWave* C::kSliceWaves) void weights_kernel(ShapedParams p) {
   const int lane = threadIdx.x & (kWave - 1);

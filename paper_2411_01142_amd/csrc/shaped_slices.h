@@ -11,6 +11,11 @@
 // Where a workgroup's wavefronts hold several shares of a pair they are merged in LDS by
 // the last of them, and only one share per workgroup and pair passes through the
 // workspace.
+//
+// A workgroup of four (bf16) or eight (packed) wavefronts per compute unit, so that each
+// holds two tiles of 8 KiB in registers without spilling; more wavefronts with one tile
+// each, K and V apart, were slower. What a call pays besides its bytes is about 10 us: two
+// reads of the lengths, the first tiles' latency, the merges.
 #pragma once
 
 #include "shaped.h"
