@@ -232,9 +232,9 @@ __device__ inline void add_weights(const ShapedParams& p, const Place& at, int32
 // for the tokens that the request sees. Reads K alone. Equal slices of the batch's steps,
 // one per wavefront, as of attention over large batches; tokens need no merging. 64 requests
 // of U[512, 2048] tokens, 32/8 heads: 32.5 us, 5.8 TB/s of keys and sums. Packed, 256 of
-// U[256, 4096], 64/8 heads, capped: 69 us, 4.9 TB/s, or 5.1 with the whole lines of which the
-// keys' exponents take half; the tanh of each score costs as much as its products. (A
-// workgroup per pair: 77.)
+// U[256, 4096], 64/8 heads, capped: 68 us, 4.9 TB/s, or 5.2 with the whole lines of which the
+// keys' exponents take half; the conversions and the caps are what is left beside the loads.
+// (A workgroup per pair: 77.)
 template <class C>
 __global__ __launch_bounds__(kWave* C::kSliceWaves) void weights_kernel(ShapedParams p) {
   const int lane = threadIdx.x & (kWave - 1);

@@ -24,7 +24,7 @@ namespace neo {
 namespace {
 
 constexpr int32_t kSlicePairCost = 1;
-constexpr int32_t kSliceMinPositions = 2;
+constexpr int32_t kSliceMinPositions = 2;  // no slice of less than a pair's cost and a step
 
 template <class C>
 __device__ inline float natural_lse(const ShapedParams& p, int32_t g, int h, const Seen& seen,
