@@ -10,9 +10,9 @@
 // One pass over a pair's tokens with the running maximum and sum of a softmax, products
 // of 16 columns (the group's heads) on the matrix cores, sums in fp32. Over bf16 caches HBM
 // bounds it (512 bytes a token and kv head; 256 requests of 64/8 heads that see 1500
-// tokens, capped: 208 us, 6.4 TB/s). Over packed ones, with 136 bytes, the conversions,
+// tokens, capped: 203 us, 6.6 TB/s). Over packed ones, with 136 bytes, the conversions,
 // the products and the softmax of a wavefront no longer hide wholly behind the loads
-// (512 requests of U[256, 4096] tokens: 222 us, 5.5 TB/s; the same loads without
+// (512 requests of U[256, 4096] tokens: 223 us, 5.5 TB/s; the same loads without
 // arithmetic 205), so what counts there is few instructions a token.
 #pragma once
 
